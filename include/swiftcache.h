@@ -148,6 +148,52 @@ typedef struct {
  * head_dim other than 64/128; SC_ERR_OOM when an allocation fails. */
 sc_status sc_pool_create(const sc_pool_desc *desc, sc_pool **out);
 
+/* How a pool's blocks hold K and V: the element type's 16 bits, or one byte
+ * per element and one scale per (token, KV head). */
+typedef enum {
+  SC_KV_16BIT = 0,
+  SC_KV_INT8 = 1,            /* codes -127..127                              */
+  SC_KV_E4M3 = 2             /* 8-bit floating point, 3 mantissa bits, no infinities, largest 448 */
+} sc_kv_format;
+
+/*
+ * A pool whose blocks hold K and V in `kv_format`: half the device and host
+ * memory of a conversation and half the bytes of every fetch.  SC_KV_16BIT
+ * is sc_pool_create.  desc->dtype stays the element type of q, K, V, the
+ * active buffers and the outputs; sc_store_layer_kv and the stacks quantise
+ * the rows they write, sc_fetch_layer_kv and the stacks turn them back into
+ * 16-bit rows, and sc_decode_attn reads them in place.  Prefill attention
+ * sees the new turn's K/V as given (the active buffer is never quantised)
+ * and the prefix as the pool holds it.
+ *
+ * A row x[0..D) of one token and KV head, a = max |x|, T = 127 (int8) or 448
+ * (e4m3):
+ *     s = max(a / T rounded up to a bf16, 2^-126),  code_d = x_d / s rounded
+ *     to the nearest code (ties to even),  value_d = code_d * s.
+ * A value is off by at most half a code step.  A code whose value would
+ * round to infinity in dtype is taken one step lower.  A row that holds a
+ * NaN or an infinity gets s = NaN and codes 0, so all of it reads as NaN.
+ * Rows are independent: writing a token into a partly filled block changes
+ * no other token.  A fetch rounds each value to dtype once (nearest even).
+ *
+ * One block of one layer (block_size B, H KV heads, head_dim D):
+ *     K codes [B][H][D], K scales bf16 [B][H], padding to 16 bytes, then V
+ *     likewise;
+ * sc_pool_layout_get gives slice_bytes = 2 * half and row_bytes = H * D (one
+ * token's codes), sc_pool_quant_get the scales' offset in a half.
+ * Errors: as sc_pool_create, plus SC_ERR_INVALID (unknown kv_format) and
+ * SC_ERR_UNSUPPORTED for n_rc_blocks > 0 with an 8-bit format (prefill
+ * attention reads regular-cache blocks in place as 16-bit rows).
+ * sc_fetch_layer_kv_dma refuses such pools (SC_ERR_UNSUPPORTED): the copy
+ * engines do not convert.
+ */
+sc_status sc_pool_create_quant(const sc_pool_desc *desc, int32_t kv_format, sc_pool **out);
+
+/* The pool's sc_kv_format, the bytes of the K (or V) half of one block of
+ * one layer and the offset of the scales in it (16-bit pools: half_bytes,
+ * none).  Each out-pointer may be NULL. */
+sc_status sc_pool_quant_get(const sc_pool *pool, int32_t *kv_format, size_t *half_bytes, size_t *scale_offset);
+
 /* Free a pool and any tiers it allocated.  Call only after every stream that
  * used it has drained.  NULL is ignored. */
 void sc_pool_destroy(sc_pool *pool);
@@ -451,6 +497,163 @@ sc_status sc_attn_plan_query(int32_t batch, const int32_t *prefix_len, const int
 sc_status sc_attn_plan_kinds(int32_t batch, const int32_t *prefix_len, const int32_t *new_len,
                              const int32_t *rc_keys, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                              int32_t slots, int32_t *narrow_rows, int32_t *merge_groups);
+
+/* ------------------------------------------------------------------------
+ * Rotary positions and decode steps.
+ * ---------------------------------------------------------------------- */
+
+/* Which elements of a head form a pair (R = rotary_dim). */
+typedef enum {
+  SC_ROPE_HALF = 0,          /* (i, i + R/2)     */
+  SC_ROPE_INTERLEAVED = 1    /* (2i, 2i + 1)     */
+} sc_rope_layout;
+
+/* How the frequencies theta_i = base^(-2i / R), i < R/2, are scaled for
+ * contexts longer than the trained one of original_len tokens. */
+typedef enum {
+  SC_ROPE_PLAIN = 0,         /* theta_i                                      */
+  SC_ROPE_LINEAR = 1,        /* theta_i / factor                             */
+  SC_ROPE_BANDED = 2,        /* by turns over the trained context,
+                                n_i = original_len * theta_i / 2 pi: theta_i from `high` turns on,
+                                theta_i / factor up to `low`, between them
+                                (1 - w) theta_i / factor + w theta_i, w = (n_i - low) / (high - low) */
+  SC_ROPE_RAMP = 3           /* by index: c(n) = R ln(original_len / (2 pi n)) / (2 ln base),
+                                lo = max(0, floor(c(high))), hi = min(R - 1, ceil(c(low))),
+                                w = (i - lo) / (hi - lo) clipped to [0, 1]: (1 - w) theta_i + w theta_i / factor */
+} sc_rope_scaling;
+
+typedef struct {
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t rotary_dim;        /* R: the first R elements of a head turn; a multiple of 16, 16..head_dim */
+  int32_t layout;            /* sc_rope_layout */
+  int32_t scaling;           /* sc_rope_scaling */
+  double base;               /* > 1 */
+  double factor;             /* > 0; SC_ROPE_PLAIN ignores it */
+  double original_len;       /* BANDED, RAMP: > 0 */
+  double low, high;          /* BANDED, RAMP: 0 < low < high */
+  double amplitude;          /* multiplies cos and sin; 0: 1, for SC_ROPE_RAMP max(1, 0.1 ln(factor) + 1) */
+  int32_t device;            /* HIP device ordinal */
+} sc_rope_desc;
+
+typedef struct sc_rope sc_rope;     /* opaque, library-owned */
+
+/* Computes the frequencies (double precision) and keeps them on the device.
+ * Errors: SC_ERR_INVALID (null, a value outside its range above, not
+ * finite), SC_ERR_UNSUPPORTED (head_dim, rotary_dim), SC_ERR_OOM. */
+sc_status sc_rope_create(const sc_rope_desc *desc, sc_rope **out);
+
+/* Call only after every stream that used it has drained.  NULL is ignored. */
+void sc_rope_destroy(sc_rope *rope);
+
+/* Host only: the scaled frequencies theta_0.. (radians per position) into
+ * theta[capacity], their number R/2 into *n; theta may be NULL.
+ * Errors: SC_ERR_INVALID (null), SC_ERR_RANGE (capacity too small). */
+sc_status sc_rope_frequencies(const sc_rope *rope, double *theta, int32_t capacity, int32_t *n);
+
+/*
+ * Rotary positions of q and k, as they are needed before sc_append_new_kv,
+ * sc_store_layer_kv and attention: for token t, head h, pair i
+ *     (x0, x1) -> a (x0 cos f - x1 sin f, x0 sin f + x1 cos f),
+ *     f = positions[t] * theta_i, a the amplitude;
+ * elements from rotary_dim on are copied.  positions: device int32
+ * [n_tokens], any values (angles are reduced in double precision, so far
+ * positions lose nothing).  q: token t's n_q_heads x head_dim elements of
+ * `dtype` start at q + t * q_stride elements (e.g. a slice of a fused
+ * projection's rows); q_out, k, k_out likewise with strides of their own.
+ * q_out == q with equal strides works in place; otherwise inputs and
+ * outputs must not overlap.  n_q_heads or n_kv_heads may be 0 (that pair of
+ * pointers is then not looked at).  Arithmetic in fp32, rounded once.
+ * Errors: SC_ERR_INVALID (null, unknown dtype, negative counts, pointers
+ * not 16-byte aligned (positions: 4), a stride that is not a multiple of 8
+ * or shorter than a token's heads), SC_ERR_RANGE (n_tokens above 2^31 - 1).
+ */
+sc_status sc_rope_apply(const sc_rope *rope, int32_t dtype, int64_t n_tokens, const int32_t *positions,
+                        const void *q, int64_t q_stride, int32_t n_q_heads, void *q_out, int64_t q_out_stride,
+                        const void *k, int64_t k_stride, int32_t n_kv_heads, void *k_out, int64_t k_out_stride,
+                        void *stream);
+
+/*
+ * One decode step of a batch over a pool: n_new tokens per sequence (1 for
+ * plain generation, up to 16 with drafted tokens).  All index
+ * arrays are device memory and are read by the kernels, so a captured step
+ * can be replayed after kv_len and block_ids have been advanced.
+ *   kv_len[b]     tokens of sequence b in its own blocks, the n_new ones of
+ *                 this step included; -1 (any negative value): an empty slot
+ *                 of a padded batch.
+ *   block_ids     [batch][max_blocks]: token t of sequence b is row
+ *                 t % block_size of block block_ids[b][t / block_size];
+ *                 entries past the length are not read.  Ids of any tier.
+ *   shared_ids    the blocks of a prefix of shared_len tokens that every
+ *                 sequence of the batch continues (a system prompt, one
+ *                 document): ceil(shared_len / block_size) ids; its last
+ *                 block may be partly filled, own tokens start in own
+ *                 blocks.  NULL when shared_len is 0.
+ *   max_len       no kv_len of this call or of a replay of it is larger.
+ * A sequence is bad when kv_len exceeds max_len or max_blocks *
+ * block_size, or an id it needs is outside the pool or not lent; that is
+ * only known on the device, where nothing outside the pool is touched:
+ * sc_decode_store skips the token, sc_decode_attn gives the sequence's rows
+ * (a bad shared id: all rows) NaN.
+ */
+typedef struct {
+  int32_t batch;
+  int32_t n_new;             /* 1..16 */
+  int32_t max_blocks;
+  int32_t max_len;
+  const int32_t *block_ids;
+  const int32_t *kv_len;
+  const int32_t *shared_ids;
+  int32_t shared_len;
+} sc_decode_batch;
+
+/*
+ * Writes the step's tokens into the pool, layer `layer`: row b * n_new + i
+ * of k_new / v_new ([batch * n_new][n_kv_heads][head_dim] of the pool's
+ * element type) becomes token kv_len[b] - n_new + i of sequence b, quantised
+ * as the pool holds it; tokens before 0 and empty slots are skipped.
+ * With `rope` (NULL: none) k_new is rotated on the way, and so is q
+ * ([batch * n_new][n_q_heads][head_dim]) into q_out (may be q), at position
+ * shared_len + kv_len[b] - n_new + i; both are rounded to the element type
+ * first, exactly as sc_rope_apply would.  q == NULL: only k.  The q_out rows
+ * of empty slots are not written.
+ * Two tokens of one call must not name the same row of the same block.
+ * Errors: SC_ERR_INVALID (null, misaligned, sizes outside their ranges, rope
+ * of another device, q without rope), SC_ERR_UNSUPPORTED (rope of another
+ * head_dim), SC_ERR_RANGE (layer; batch * n_new * heads beyond 2^31 - 1).
+ */
+sc_status sc_decode_store(sc_pool *pool, int32_t layer, const sc_decode_batch *batch, const void *k_new,
+                          const void *v_new, const sc_rope *rope, const void *q, int32_t n_q_heads, void *q_out,
+                          void *stream);
+
+/* Host only: bytes of device workspace that sc_decode_attn needs for this
+ * batch (pointers in it are not looked at).  Errors: as sc_decode_attn. */
+sc_status sc_decode_workspace(const sc_pool *pool, const sc_decode_batch *batch, int32_t n_q_heads, size_t *bytes);
+
+/*
+ * Attention of a decode step over the pool in place: row (b, i) of q
+ * ([batch * n_new][n_q_heads][head_dim]) attends to all shared_len shared
+ * tokens and to the own tokens t < kv_len[b] - n_new + i + 1 of its sequence
+ * at layer `layer`, whose K/V must be in the pool (sc_decode_store), softmax
+ * and GQA as sc_prefill_attn (scale <= 0: 1/sqrt(head_dim)).  The shared
+ * tokens' K/V are read once for the whole batch.  out like q; lse
+ * (nullable): float [n_q_heads][batch * n_new].  A row without any key
+ * gives zeros and lse -infinity, and so do empty slots' rows; what keys that
+ * a row does not see hold, NaN included, does not reach it.
+ * K and V are used as the pool holds them (no 16-bit copy is rounded);
+ * scores, softmax and outputs accumulate in fp32, the probabilities of the
+ * PV product are rounded to 16 bits, the output once.
+ * The call allocates nothing and enqueues kernels only, so it can be
+ * captured; `workspace` (256-byte aligned, workspace_bytes of at least
+ * sc_decode_workspace) belongs to the call until it has completed: calls
+ * that may overlap, and captured graphs, need workspaces of their own.
+ * Errors: SC_ERR_INVALID (null, misaligned, sizes outside their ranges, a
+ * workspace too small), SC_ERR_UNSUPPORTED (GQA group > 16), SC_ERR_RANGE
+ * (layer; batch * n_new * n_q_heads beyond 2^31 - 1, or more than 2^31 - 257
+ * shared or own tokens).
+ */
+sc_status sc_decode_attn(sc_pool *pool, int32_t layer, const sc_decode_batch *batch, const void *q,
+                         int32_t n_q_heads, float scale, void *out, float *lse, void *workspace,
+                         size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
  * Elastic donor tier and capacity planning (host only, no device work).

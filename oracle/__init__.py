@@ -20,6 +20,9 @@ Contents
               §5 "Model": GQA).
 ``capacity``  the master's layer stream cache and regular cache sizes and
               the longest supported context (§3.2, Eq. 1-5).
+``decode``    8-bit KV rows, rotary positions and the attention of a decode
+              step over a prefix the batch shares and each sequence's own
+              tokens.
 ``elastic``   the worker's elastic cache: layer-major vs block-major resize
               moves, the minimum elastic unit (Eq. 6-9) and the scale-up /
               scale-down decisions of Algorithm 1 (§3.4-§3.5).
@@ -33,4 +36,4 @@ docstrings for which pin covers which function.  No function is "parity
 unpinned".
 """
 
-from . import attention, capacity, elastic, kvcache  # noqa: F401
+from . import attention, capacity, decode, elastic, kvcache  # noqa: F401

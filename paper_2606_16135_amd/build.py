@@ -19,7 +19,8 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 LIB_NAME = "libswiftcache.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 
-SOURCES = ["sc_api.cpp", "sc_elastic.cpp", "kv_copy.hip", "attn_fwd.hip"]
+SOURCES = ["sc_api.cpp", "sc_elastic.cpp", "sc_decode.cpp", "kv_copy.hip", "kv8_copy.hip", "attn_fwd.hip",
+           "rope.hip", "decode_attn.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 instructions are disabled for all device code: some of their

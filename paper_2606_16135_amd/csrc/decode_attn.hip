@@ -1,0 +1,847 @@
+// Attention of a decode step over the pool in place (sc_decode_attn): few
+// query rows per sequence, keys and values read through block lists from
+// wherever the blocks are, 16-bit or 8-bit, and a prefix shared by the whole
+// batch read once.
+//
+//     o = sum_j softmax_j(scale * q . k_j) v_j
+//
+// over the shared keys and the row's own.  A row's keys are cut into chunks;
+// every chunk gives a partial (maximum m, sum l = sum 2^(s_j - m), O = sum
+// 2^(s_j - m) v_j, all fp32) and decode_merge_kernel joins them: with M the
+// largest m, o = sum 2^(m - M) O / sum 2^(m - M) l.  One chunk in all and no
+// shared prefix: the first kernel writes the result itself.
+//
+// decode_narrow_kernel: up to 16 rows of one KV head (the tokens and query
+// heads of one sequence) against one chunk, bound by reading K and V once:
+// 16 rows take the matrix units 16 cycles for 2 KiB (16-bit) that HBM
+// delivers to a CU in 230.  K and V go from memory straight into the operand
+// registers, with no LDS between, because no two waves share a key:
+//   S^T (16 keys x 16 rows) = K . Q^T   lane (m = l % 16, g = l / 16) holds
+//       key m's elements of its slots; which elements of the head a slot
+//       stands for is free as long as Q^T uses the same, so a lane takes 16
+//       contiguous bytes;
+//   O^T (16 dims x 16 rows) += V^T . P^T   the slots of lane group g are the
+//       8 keys whose scores that group already holds, so P needs no
+//       exchange between lanes, and the dims of operand d are D / 16 * m + d:
+//       a lane loads D / 16 contiguous elements of 8 keys and the D / 16
+//       operands are that square transposed in registers.
+// A wave takes 64 keys at a time (up to 32 KiB of loads in flight), the four
+// waves of a workgroup take turns, and join their partials through LDS.
+//
+// decode_wide_kernel: more rows than that share the keys (a shared prefix:
+// every row of the batch).  A workgroup of four waves of 32 rows takes
+// 128-key tiles through LDS: the tile is loaded to registers while the one
+// before is computed, then converted to 16 bits (8-bit codes are exact in
+// bf16 and fp16) and written to LDS in operand order, so that the key loop
+// reads whole 16-byte operands and an 8-bit tile is converted once for all
+// rows.
+//
+// 8-bit K and V: a key's scales are applied to its score and to its
+// probability, in fp32.  The probabilities are rounded to the element type
+// for the PV product, with 8-bit blocks always to bf16: scaled by a row's
+// scale they may be far below what fp16 holds, and the codes need 8 bits.
+//
+// Keys past a row's end: scores are replaced by -infinity (never computed
+// with), probabilities by 0 after scaling, and where such keys are in a tile
+// at all the V operands are zeroed as well, per token of the step where the
+// tokens' ends differ, so that nothing a hidden key holds (0 x NaN) arrives.
+#include "sc_internal.h"
+#include "sc_pool_view.h"
+#include "sc_quant.h"
+
+#include <atomic>
+
+namespace sc {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kStep = 64;             // keys of a wave's step (narrow)
+constexpr int kTile = 128;            // keys of a workgroup's tile (wide)
+constexpr int kWideRows = 128;
+constexpr float kNegInf = -__builtin_inff();
+
+template <int DT>
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  if constexpr (DT == SC_DTYPE_BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// Geometry of one (head_dim, format): a head's row in memory and the pieces
+// a lane takes of it.
+template <int D, int FMT>
+struct Geo {
+  static constexpr bool k8 = FMT != SC_KV_16BIT;
+  static constexpr int kElem = k8 ? 1 : 2;
+  static constexpr int kRow = D * kElem;                 // bytes of one head's row
+  static constexpr int kSteps = D / 32;                  // MFMA steps of a score
+  static constexpr int kLoads = kRow / 64;               // 16-byte K loads of a lane
+  static constexpr int kVd = D / 16;                     // dims a lane takes of a V row
+  static constexpr int kVWords = kVd * kElem / 4;        // ... in 32-bit words
+};
+
+// First head element of lane group g's slots in MFMA step c.
+template <int D, int FMT>
+__device__ __forceinline__ int slot_dim(int c, int g) {
+  return Geo<D, FMT>::k8 ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
+}
+
+template <int N>
+struct Words {
+  uint32_t w[N];
+};
+template <int N>
+__device__ __forceinline__ Words<N> load_words(const char *p) {
+  Words<N> r;
+  if constexpr (N == 1) {
+    r.w[0] = *reinterpret_cast<const uint32_t *>(p);
+  } else if constexpr (N == 2) {
+    const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+    r.w[0] = v.x, r.w[1] = v.y;
+  } else {
+    const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+    r.w[0] = v.x, r.w[1] = v.y, r.w[2] = v.z, r.w[3] = v.w;
+  }
+  return r;
+}
+
+// K operands of one key: D / 32 steps from its loads.
+template <int D, int FMT, int DT>
+__device__ __forceinline__ u32x4 k_operand(const u32x4 (&raw)[Geo<D, FMT>::kLoads], int c) {
+  if constexpr (!Geo<D, FMT>::k8) {
+    return raw[c];
+  } else {
+    u32x4 r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float f[4];
+      codes_to_f32<FMT>(raw[c >> 1][2 * (c & 1) + h], f);
+      r[2 * h] = pack16<DT>(f[0], f[1]);
+      r[2 * h + 1] = pack16<DT>(f[2], f[3]);
+    }
+    return r;
+  }
+}
+
+// V operands of 8 keys: operand d holds dim d of every key.
+template <int D, int FMT>
+__device__ __forceinline__ void v_operands(const Words<Geo<D, FMT>::kVWords> (&raw)[8], u32x4 (&op)[D / 16]) {
+  using G = Geo<D, FMT>;
+  if constexpr (!G::k8) {
+#pragma unroll
+    for (int w = 0; w < G::kVWords; ++w)
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const uint32_t a = raw[2 * p].w[w], b = raw[2 * p + 1].w[w];
+        op[2 * w][p] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+        op[2 * w + 1][p] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+      }
+  } else {
+#pragma unroll
+    for (int w = 0; w < G::kVWords; ++w)
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        float a[4], b[4];
+        codes_to_f32<FMT>(raw[2 * p].w[w], a);
+        codes_to_f32<FMT>(raw[2 * p + 1].w[w], b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) op[4 * w + i][p] = pack16<SC_DTYPE_BF16>(a[i], b[i]);
+      }
+  }
+}
+
+// Element type of the PV product.
+template <int FMT, int DT>
+constexpr int pv_type() {
+  return FMT == SC_KV_16BIT ? DT : SC_DTYPE_BF16;
+}
+
+// Keys of sequence b in its own blocks; -1 for an empty slot, kBad for a
+// length beyond the call's bounds.
+constexpr int kBad = -2;
+__device__ __forceinline__ int own_len(const DecodeAttnArgs &a, int b) {
+  const int len = a.batch.kv_len[b];
+  if (len < 0) return -1;
+  return len > a.batch.max_len || len > (int64_t)a.batch.max_blocks * a.pool.block_size ? kBad : len;
+}
+
+// LDS that only one wave uses: its accesses are executed in order, so only
+// the compiler has to keep them so.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Running softmax of one row (one lane column): reference max, this lane's
+// part of the sum.
+struct RowState {
+  float m, l;
+};
+
+// p = 2^(x - m) for the lane's N scores of one row; the row's four lanes
+// agree on m.  Returns the factor for what was accumulated before.
+template <int N>
+__device__ __forceinline__ float softmax_step(float (&x)[N], RowState &st) {
+  float top = x[0];
+#pragma unroll
+  for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+  top = fmaxf(top, __shfl_xor(top, 16));
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float m = fmaxf(st.m, top);
+  const float ref = m == kNegInf ? 0.f : m;
+  const float alpha = __builtin_amdgcn_exp2f(st.m - ref);
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
+    sum += x[i];
+  }
+  st.l = st.l * alpha + sum;
+  st.m = m;
+  return alpha;
+}
+
+// Writes of one row's 8 (head_dim 64: 4) consecutive dims.
+template <int N>
+__device__ __forceinline__ void store_f32(float *p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4) *reinterpret_cast<f32x4 *>(p + i) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+}
+
+// ---------------------------------------------------------------------------
+// Narrow: one chunk of one sequence's own keys (SHARED: of the shared ones),
+// one KV head, 16 rows.  Blocks are ordered (sequence, chunk, row tile, KV
+// head): the row tiles of a chunk land on one XCD when there are 8 KV heads
+// and read its L2.
+// ---------------------------------------------------------------------------
+template <int D, int FMT, int DT, bool SHARED>
+__global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnArgs a, int row_tiles) {
+  using G = Geo<D, FMT>;
+  constexpr int kPv = pv_type<FMT, DT>();
+  __shared__ __attribute__((aligned(16))) uint64_t s_addr[kWaves][kStep];
+  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][2][kStep];
+  __shared__ float s_ml[kWaves][16][2], s_row[16][2];
+  __shared__ __attribute__((aligned(16))) float s_o[kWaves][16][D];
+  __shared__ int s_bad;
+
+  const PoolView &p = a.pool;
+  int id = blockIdx.x;
+  const int kvh = id % p.n_kv_heads;
+  id /= p.n_kv_heads;
+  const int tile = id % row_tiles;
+  id /= row_tiles;
+  const int n_chunks = SHARED ? a.plan.shared_chunks : a.plan.own_chunks;
+  const int chunk = id % n_chunks;
+  const int seq = SHARED ? 0 : id / n_chunks;
+
+  const int group = a.plan.group;
+  const int n_new = a.batch.n_new;
+  const int len = SHARED ? a.batch.shared_len : own_len(a, seq);
+  const int size = SHARED ? a.plan.shared_chunk : a.plan.own_chunk;
+  const int k0 = chunk * size;
+  const int k1 = min(len, k0 + size);
+  const bool direct = a.plan.direct != 0;
+  if (k0 >= k1 && !direct) return;           // the merge counts the chunks that hold keys
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int n = lane & 15, g = lane >> 4;
+  const int rows = SHARED ? a.plan.tokens * group : n_new * group;
+  const int row = tile * 16 + n;             // this lane's column
+  const bool has_row = row < rows;
+  const int tok_in = has_row ? row / group : 0;              // token of the step (SHARED: of the batch)
+  const int token = SHARED ? tok_in : seq * n_new + tok_in;
+  const int head = kvh * group + (has_row ? row - tok_in * group : 0);
+  const int limit = SHARED ? len : len - n_new + tok_in + 1; // keys below it are the row's
+
+  // Q^T operands.
+  u32x4 qf[G::kSteps];
+  const uint16_t *qrow = a.q + ((int64_t)token * a.n_q_heads + head) * D;
+#pragma unroll
+  for (int c = 0; c < G::kSteps; ++c)
+    qf[c] = has_row ? *reinterpret_cast<const u32x4 *>(qrow + slot_dim<D, FMT>(c, g)) : u32x4{0, 0, 0, 0};
+
+  if (threadIdx.x == 0) s_bad = len == kBad ? 1 : 0;
+  __syncthreads();
+
+  const int32_t *ids = SHARED ? a.batch.shared_ids : a.batch.block_ids + (int64_t)seq * a.batch.max_blocks;
+  const int64_t head_off = (int64_t)kvh * G::kRow;
+  const int64_t row_bytes = (int64_t)p.n_kv_heads * G::kRow;
+  // Keys from here on are hidden from some row of the tile.
+  const int first_tok = tile * 16 / group;
+  const int min_limit = SHARED ? len : len - n_new + first_tok + 1;
+
+  RowState st = {kNegInf, 0.f};
+  f32x4 o[G::kVd];
+#pragma unroll
+  for (int d = 0; d < G::kVd; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  int base = k0 + wave * kStep;
+  int32_t next_id = 0;
+  if (base < k1) next_id = ids[block_of(p, min(base + lane, k1 - 1))];
+  for (; base < k1; base += kWaves * kStep) {
+    const int key = min(base + lane, k1 - 1);
+    const char *blk = block_layer(p, next_id);
+    const int in_block = key - block_of(p, key) * p.block_size;
+    if (base + kWaves * kStep < k1) next_id = ids[block_of(p, min(base + kWaves * kStep + lane, k1 - 1))];
+    if (__any(blk == nullptr)) {             // an id outside the pool: nothing of it is read
+      s_bad = 1;
+      break;
+    }
+    const char *krow = blk + in_block * row_bytes + head_off;
+    uint32_t ks = 0, vs = 0;
+    if constexpr (G::k8) {
+      const char *sp = blk + p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
+      ks = *reinterpret_cast<const uint16_t *>(sp);
+      vs = *reinterpret_cast<const uint16_t *>(sp + p.half_bytes);
+    }
+    s_addr[wave][lane] = reinterpret_cast<uint64_t>(krow);
+    wave_lds_order();
+
+    u32x4 kr[4][G::kLoads];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const char *kp = reinterpret_cast<const char *>(s_addr[wave][16 * t + n]) + 16 * g;
+#pragma unroll
+      for (int c = 0; c < G::kLoads; ++c) kr[t][c] = *reinterpret_cast<const u32x4 *>(kp + 64 * c);
+    }
+    Words<G::kVWords> vr[2][8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const char *vp = reinterpret_cast<const char *>(s_addr[wave][32 * u + 16 * (j >> 2) + 4 * g + (j & 3)]);
+        vr[u][j] = load_words<G::kVWords>(vp + p.half_bytes + n * (G::kVd * G::kElem));
+      }
+
+    if constexpr (G::k8) {                   // only now: the scales' loads are older than the ones above
+      s_scale[wave][0][lane] = __builtin_bit_cast(float, ks << 16);
+      s_scale[wave][1][lane] = __builtin_bit_cast(float, vs << 16);
+      wave_lds_order();
+    }
+
+    // Scores of 64 keys: lane (n, g) gets keys 16 t + 4 g + i of row n.
+    float x[16];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < G::kSteps; ++c) s = mfma16<DT>(k_operand<D, FMT, DT>(kr[t], c), qf[c], s);
+      f32x4 sc = {1.f, 1.f, 1.f, 1.f};
+      if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&s_scale[wave][0][16 * t + 4 * g]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * t + i] = s[i] * (G::k8 ? sc[i] * a.scale_log2 : a.scale_log2);
+    }
+    const bool edge = base + kStep > min(k1, min_limit);   // the same for the whole wave
+    if (edge) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (base + 16 * t + 4 * g + i >= min(limit, k1)) x[4 * t + i] = kNegInf;
+    }
+    const float alpha = softmax_step(x, st);
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int d = 0; d < G::kVd; ++d) o[d] *= alpha;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      u32x4 pf;
+      float w[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x4 sc = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&s_scale[wave][1][32 * u + 16 * h + 4 * g]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[4 * h + i] = x[8 * u + 4 * h + i];
+          if constexpr (G::k8) w[4 * h + i] *= sc[i];
+        }
+      }
+      if (G::k8 && edge) {                   // 0 x a hidden key's NaN scale
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (base + 32 * u + 16 * (j >> 2) + 4 * g + (j & 3) >= min(limit, k1)) w[j] = 0.f;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) pf[q] = pack16<kPv>(w[2 * q], w[2 * q + 1]);
+      u32x4 vo[G::kVd];
+      if (!edge) {
+        v_operands<D, FMT>(vr[u], vo);
+#pragma unroll
+        for (int d = 0; d < G::kVd; ++d) o[d] = mfma16<kPv>(vo[d], pf, o[d]);
+      } else {
+        // One pass per distinct end: V without the keys that this token does
+        // not see, added to its rows only.
+        const int last_tok = SHARED ? first_tok : min(n_new - 1, (tile * 16 + 15) / group);
+        for (int tk = first_tok; tk <= last_tok; ++tk) {
+          const int end = min(k1, SHARED ? len : len - n_new + tk + 1);
+          Words<G::kVWords> cut[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool hidden = base + 32 * u + 16 * (j >> 2) + 4 * g + (j & 3) >= end;
+#pragma unroll
+            for (int q = 0; q < G::kVWords; ++q) cut[j].w[q] = hidden ? 0u : vr[u][j].w[q];
+          }
+          v_operands<D, FMT>(cut, vo);
+          const bool mine = SHARED || tok_in == tk;
+#pragma unroll
+          for (int d = 0; d < G::kVd; ++d) {
+            const f32x4 add = mfma16<kPv>(vo[d], pf, f32x4{0.f, 0.f, 0.f, 0.f});
+            if (mine) o[d] += add;
+          }
+        }
+      }
+    }
+    wave_lds_order();
+  }
+
+  // Join the four waves.
+  st.l += __shfl_xor(st.l, 16);
+  st.l += __shfl_xor(st.l, 32);
+  if (g == 0) {
+    s_ml[wave][n][0] = st.m;
+    s_ml[wave][n][1] = st.l;
+  }
+  __syncthreads();
+  float m = kNegInf, l = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_ml[w][n][0]);
+  const float ref = m == kNegInf ? 0.f : m;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) l += s_ml[w][n][1] * __builtin_amdgcn_exp2f(s_ml[w][n][0] - ref);
+  const float f = __builtin_amdgcn_exp2f(st.m - ref);
+  // o[d][i]: dim G::kVd * (4 g + i) + d of row n.
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float v[G::kVd];
+#pragma unroll
+    for (int d = 0; d < G::kVd; ++d) v[d] = o[d][i] * f;
+    store_f32(&s_o[wave][n][G::kVd * (4 * g + i)], v);
+  }
+  if (wave == 0 && g == 0) {
+    s_row[n][0] = m;
+    s_row[n][1] = l;
+  }
+  __syncthreads();
+  const bool bad = s_bad != 0;
+  const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
+  const int part = SHARED ? chunk : a.plan.shared_chunks + chunk;
+  // Thread: 4 dims of a row; 16 rows x D / 4 threads' worth.
+  for (int idx = threadIdx.x; idx < 16 * (D / 4); idx += kThreads) {
+    const int r = idx / (D / 4), d0 = 4 * (idx % (D / 4));
+    const int rr = tile * 16 + r;
+    if (rr >= rows) continue;
+    const int tk = rr / group;
+    const int64_t out_row = (int64_t)(SHARED ? tk : seq * n_new + tk) * a.n_q_heads + kvh * group + (rr - tk * group);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4 *>(&s_o[w][r][d0]);
+    float rm = s_row[r][0], rl = s_row[r][1];
+    if (bad) rm = rl = __builtin_nanf("");
+    if (!direct) {
+      *reinterpret_cast<f32x4 *>(a.part_o + ((int64_t)part * all_rows + out_row) * D + d0) = v;
+      if (d0 == 0) a.part_ml[(int64_t)part * all_rows + out_row] = float2{rm, rl};
+    } else {
+      // No key at all: zeros.
+      const bool none = !bad && len - n_new + tk + 1 <= 0;
+      const float inv = none ? 0.f : 1.f / rl;
+      u32x2 w;
+      w.x = none ? 0u : pack16<DT>(v[0] * inv, v[1] * inv);
+      w.y = none ? 0u : pack16<DT>(v[2] * inv, v[3] * inv);
+      *reinterpret_cast<u32x2 *>(a.out + out_row * D + d0) = w;
+      if (d0 == 0 && a.lse != nullptr)
+        a.lse[(int64_t)(out_row % a.n_q_heads) * a.plan.tokens + out_row / a.n_q_heads] =
+            none ? kNegInf : (rm + __builtin_log2f(rl)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Wide: one chunk of the shared keys, one KV head, 128 rows of the batch.
+// ---------------------------------------------------------------------------
+template <int D, int FMT, int DT>
+__global__ __launch_bounds__(kThreads, 2) void decode_wide_kernel(DecodeAttnArgs a, int row_tiles) {
+  using G = Geo<D, FMT>;
+  constexpr int kPv = pv_type<FMT, DT>();
+  constexpr int kKPer = kTile * G::kRow / 16 / kThreads;      // 16-byte K pieces of a thread
+  constexpr int kPieces = G::kRow / 16;                       // ... of a key
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  u32x4 *const s_k = reinterpret_cast<u32x4 *>(smem);         // [8][D / 32][64] operands
+  u32x4 *const s_v = s_k + kTile * D / 8;                     // [4][D / 16][64]
+  uint64_t(*const s_addr)[kTile] = reinterpret_cast<uint64_t(*)[kTile]>(s_v + kTile * D / 8);   // [2]
+  float(*const s_scale)[kTile] = reinterpret_cast<float(*)[kTile]>(s_addr + 2);                 // [2]: K, V
+  int *const s_bad = reinterpret_cast<int *>(s_scale + 2);   // [2], tiles of one parity: set while the other is read
+
+  const PoolView &p = a.pool;
+  int id = blockIdx.x;
+  const int kvh = id % p.n_kv_heads;
+  id /= p.n_kv_heads;
+  const int tile = id % row_tiles;
+  const int chunk = id / row_tiles;
+  const int group = a.plan.group;
+  const int k0 = chunk * a.plan.shared_chunk;
+  const int k1 = min(a.batch.shared_len, k0 + a.plan.shared_chunk);
+  const int tiles = (k1 - k0 + kTile - 1) / kTile;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = lane & 15, g = lane >> 4;
+  const int rows = a.plan.tokens * group;
+  const int row0 = tile * kWideRows + wave * 32;
+  const bool busy = row0 < rows;             // this wave has rows
+  int64_t out_row[2];
+  bool has_row[2];
+  u32x4 qf[2][G::kSteps];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int row = row0 + 16 * r + n;
+    has_row[r] = row < rows;
+    const int token = has_row[r] ? row / group : 0;
+    out_row[r] = (int64_t)token * a.n_q_heads + kvh * group + (has_row[r] ? row - token * group : 0);
+#pragma unroll
+    for (int c = 0; c < G::kSteps; ++c)
+      qf[r][c] = has_row[r] ? *reinterpret_cast<const u32x4 *>(a.q + out_row[r] * D + slot_dim<D, FMT>(c, g))
+                            : u32x4{0, 0, 0, 0};
+  }
+
+  const int64_t head_off = (int64_t)kvh * G::kRow;
+  const int64_t row_bytes = (int64_t)p.n_kv_heads * G::kRow;
+  const int my_key = tid & (kTile - 1);      // threads 0..127: K's scale, 128..255: V's
+  if (tid < 2) s_bad[tid] = 0;
+  __syncthreads();
+  int32_t next_id = 0;                       // block of this thread's key of the tile to address next
+  auto fetch_id = [&](int t) { next_id = a.batch.shared_ids[block_of(p, min(k0 + t * kTile + my_key, k1 - 1))]; };
+  const char *my_scale = nullptr;            // of the tile whose address was taken last
+  auto take_addr = [&](int t) {              // address of this thread's key of tile t
+    const int key = min(k0 + t * kTile + my_key, k1 - 1);
+    const char *base = block_layer(p, next_id);
+    if (base == nullptr) {
+      s_bad[t & 1] = 1;
+      return;
+    }
+    const int in_block = key - block_of(p, key) * p.block_size;
+    if (tid < kTile) s_addr[t & 1][my_key] = reinterpret_cast<uint64_t>(base + in_block * row_bytes + head_off);
+    if constexpr (G::k8)
+      my_scale = base + (tid < kTile ? 0 : p.half_bytes) + p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
+  };
+  u32x4 kr[kKPer];
+  Words<G::kVWords> vr[8];
+  uint32_t scale_bits = 0;
+  auto load_tile = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < kKPer; ++i) {
+      const int idx = tid + kThreads * i;
+      kr[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(s_addr[t & 1][idx / kPieces]) +
+                                               16 * (idx % kPieces));
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      vr[j] = load_words<G::kVWords>(
+          reinterpret_cast<const char *>(s_addr[t & 1][32 * wave + 16 * (j >> 2) + 4 * g + (j & 3)]) + p.half_bytes +
+          n * (G::kVd * G::kElem));
+    if constexpr (G::k8) scale_bits = *reinterpret_cast<const uint16_t *>(my_scale);
+  };
+  // Position of lane (m, g)'s K operand of step c: rotated among the 16 keys
+  // so that the pieces of one key, which consecutive threads write, fall on
+  // different banks.
+  auto k_slot = [&](int t16, int c, int g_, int m_) {
+    return (t16 * G::kSteps + c) * 64 + g_ * 16 + (m_ ^ ((4 * c + g_) & 15));
+  };
+  auto write_tile = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < kKPer; ++i) {
+      const int idx = tid + kThreads * i;
+      const int key = idx / kPieces, x = idx % kPieces;
+      if constexpr (!G::k8) {
+        s_k[k_slot(key >> 4, x >> 2, x & 3, key & 15)] = kr[i];
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float f0[4], f1[4];
+          codes_to_f32<FMT>(kr[i][2 * h], f0);
+          codes_to_f32<FMT>(kr[i][2 * h + 1], f1);
+          s_k[k_slot(key >> 4, 2 * (x >> 2) + h, x & 3, key & 15)] =
+              u32x4{pack16<DT>(f0[0], f0[1]), pack16<DT>(f0[2], f0[3]), pack16<DT>(f1[0], f1[1]),
+                    pack16<DT>(f1[2], f1[3])};
+        }
+      }
+    }
+    if (k0 + (t + 1) * kTile > k1) {         // no value for the keys behind the last: not a copy of its
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (k0 + t * kTile + 32 * wave + 16 * (j >> 2) + 4 * g + (j & 3) >= k1)
+#pragma unroll
+          for (int q = 0; q < G::kVWords; ++q) vr[j].w[q] = 0;
+    }
+    u32x4 vo[G::kVd];
+    v_operands<D, FMT>(vr, vo);
+#pragma unroll
+    for (int d = 0; d < G::kVd; ++d) s_v[(wave * G::kVd + d) * 64 + lane] = vo[d];
+    if constexpr (G::k8) s_scale[tid / kTile][my_key] = __builtin_bit_cast(float, scale_bits << 16);
+  };
+
+  RowState st[2] = {{kNegInf, 0.f}, {kNegInf, 0.f}};
+  f32x4 o[2][G::kVd];
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int d = 0; d < G::kVd; ++d) o[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  fetch_id(0);
+  take_addr(0);
+  if (tiles > 1) fetch_id(1);
+  __syncthreads();
+  bool bad = s_bad[0] != 0;
+  if (!bad) {
+    load_tile(0);
+    if (tiles > 1) take_addr(1);
+  }
+  for (int t = 0; t < tiles && !bad; ++t) {
+    if (t + 2 < tiles) fetch_id(t + 2);      // older than the loads below, so that waiting for it leaves them in flight
+    __syncthreads();                         // the operands of tile t - 1 have been read
+    write_tile(t);
+    __syncthreads();
+    const bool next_bad = s_bad[(t + 1) & 1] != 0;
+    if (t + 1 < tiles && !next_bad) load_tile(t + 1);
+    if (busy) {
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {          // 64 keys at a time
+        float x[2][16];
+#pragma unroll
+        for (int tt = 0; tt < 4; ++tt) {
+          f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+          for (int c = 0; c < G::kSteps; ++c) {
+            const u32x4 kf = s_k[k_slot(4 * h + tt, c, g, n)];
+            s[0] = mfma16<DT>(kf, qf[0][c], s[0]);
+            s[1] = mfma16<DT>(kf, qf[1][c], s[1]);
+          }
+          f32x4 sc = {a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
+          if constexpr (G::k8) sc *= *reinterpret_cast<const f32x4 *>(&s_scale[0][64 * h + 16 * tt + 4 * g]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            x[0][4 * tt + i] = s[0][i] * sc[i];
+            x[1][4 * tt + i] = s[1][i] * sc[i];
+          }
+        }
+        const int base = k0 + t * kTile + 64 * h;
+        const bool edge = base + 64 > k1;
+        if (edge) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (base + 16 * (i >> 2) + 4 * g + (i & 3) >= k1) x[0][i] = x[1][i] = kNegInf;
+        }
+        u32x4 pf[2][2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float alpha = softmax_step(x[r], st[r]);
+          if (__any(alpha != 1.f)) {
+#pragma unroll
+            for (int d = 0; d < G::kVd; ++d) o[r][d] *= alpha;
+          }
+          if constexpr (G::k8) {
+#pragma unroll
+            for (int tt = 0; tt < 4; ++tt) {
+              const f32x4 sc = *reinterpret_cast<const f32x4 *>(&s_scale[1][64 * h + 16 * tt + 4 * g]);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) x[r][4 * tt + i] *= sc[i];
+            }
+            if (edge) {                      // 0 x a NaN scale
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                if (base + 16 * (i >> 2) + 4 * g + (i & 3) >= k1) x[r][i] = 0.f;
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) pf[r][u][q] = pack16<kPv>(x[r][8 * u + 2 * q], x[r][8 * u + 2 * q + 1]);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int d = 0; d < G::kVd; ++d) {
+            const u32x4 vf = s_v[((2 * h + u) * G::kVd + d) * 64 + lane];
+            o[0][d] = mfma16<kPv>(vf, pf[0][u], o[0][d]);
+            o[1][d] = mfma16<kPv>(vf, pf[1][u], o[1][d]);
+          }
+      }
+    }
+    bad = next_bad;
+    if (!bad && t + 2 < tiles) take_addr(t + 2);
+  }
+
+  const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    float l = st[r].l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (!has_row[r]) continue;
+    const int64_t at = (int64_t)chunk * all_rows + out_row[r];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v[G::kVd];
+#pragma unroll
+      for (int d = 0; d < G::kVd; ++d) v[d] = o[r][d][i];
+      store_f32(a.part_o + at * D + G::kVd * (4 * g + i), v);
+    }
+    if (g == 0) a.part_ml[at] = bad ? float2{__builtin_nanf(""), __builtin_nanf("")} : float2{st[r].m, l};
+  }
+}
+
+template <int D>
+constexpr size_t wide_lds_bytes() {
+  return 2 * (size_t)kTile * D * 2 + 2 * kTile * sizeof(uint64_t) + 2 * kTile * sizeof(float) + 16;
+}
+
+// ---------------------------------------------------------------------------
+// Merge.  D / 4 lanes hold a row's output, 4 dims each; `split` such lane
+// groups of a workgroup share one row's partials.
+// ---------------------------------------------------------------------------
+template <int D, int DT>
+__global__ __launch_bounds__(kThreads) void decode_merge_kernel(DecodeAttnArgs a, int split) {
+  constexpr int kLanes = D / 4, kSlots = kThreads / kLanes;
+  __shared__ __attribute__((aligned(16))) float s_o[kSlots][D];
+  __shared__ float s_ml[kSlots][2];
+  const int slot = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
+  const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
+  const int64_t row = (int64_t)blockIdx.x * (kSlots / split) + slot / split;
+  const bool in = row < all_rows;
+  const int token = in ? (int)(row / a.n_q_heads) : 0, head = in ? (int)(row - (int64_t)token * a.n_q_heads) : 0;
+  const int seq = token / a.batch.n_new;
+  const int len = own_len(a, seq);
+  const int limit = len - a.batch.n_new + (token - seq * a.batch.n_new) + 1;
+  const int own = len > 0 ? (len + a.plan.own_chunk - 1) / a.plan.own_chunk : 0;
+  const int parts = in && len >= 0 ? a.plan.shared_chunks + own : 0;
+
+  float m = kNegInf, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  constexpr int kAhead = 4;
+  for (int p = slot % split; p < parts; p += split * kAhead) {
+    float2 ml[kAhead];
+    f32x4 v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const bool have = p + i * split < parts;
+      const int64_t at = (int64_t)(have ? p + i * split : p) * all_rows + row;
+      ml[i] = a.part_ml[at];
+      v[i] = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + d0);
+      if (!have) ml[i] = float2{kNegInf, 0.f}, v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) top = fmaxf(top, ml[i].x);
+    const float ref = top == kNegInf ? 0.f : top;
+    const float f = __builtin_amdgcn_exp2f(m - ref);
+    l *= f;
+    o *= f;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const float w = __builtin_amdgcn_exp2f(ml[i].x - ref);
+      l += w * ml[i].y;
+      o += w * v[i];
+    }
+    m = top;
+  }
+  if (split > 1) {
+    *reinterpret_cast<f32x4 *>(&s_o[slot][d0]) = o;
+    if (d0 == 0) s_ml[slot][0] = m, s_ml[slot][1] = l;
+    __syncthreads();
+    if (slot % split != 0) return;
+    for (int j = 0; j < split; ++j) m = fmaxf(m, s_ml[slot + j][0]);
+    const float ref = m == kNegInf ? 0.f : m;
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < split; ++j) {
+      const float w = __builtin_amdgcn_exp2f(s_ml[slot + j][0] - ref);
+      l += w * s_ml[slot + j][1];
+      o += w * *reinterpret_cast<const f32x4 *>(&s_o[slot + j][d0]);
+    }
+  }
+  if (!in) return;
+  const bool none = len == -1 || (len >= 0 && limit <= 0 && a.batch.shared_len == 0);
+  if (len == kBad) l = __builtin_nanf("");
+  const float inv = 1.f / l;
+  u32x2 w;
+  w.x = none ? 0u : pack16<DT>(o[0] * inv, o[1] * inv);
+  w.y = none ? 0u : pack16<DT>(o[2] * inv, o[3] * inv);
+  *reinterpret_cast<u32x2 *>(a.out + row * D + d0) = w;
+  if (d0 == 0 && a.lse != nullptr)
+    a.lse[(int64_t)head * a.plan.tokens + token] = none ? kNegInf : (m + __builtin_log2f(l)) * 0.6931471805599453f;
+}
+
+template <int D, int FMT, int DT>
+hipError_t launch_all(const DecodeAttnArgs &a, hipStream_t stream) {
+  const DecodePlan &pl = a.plan;
+  const int heads = a.pool.n_kv_heads;
+  if (pl.shared_chunks > 0) {
+    const int rows = pl.tokens * pl.group;
+    if (pl.shared_wide) {
+      constexpr size_t lds = wide_lds_bytes<D>();
+      const void *kernel = reinterpret_cast<const void *>(&decode_wide_kernel<D, FMT, DT>);
+      static std::atomic<uint64_t> ready{0};   // devices on which the kernel may use that much LDS
+      int dev = 0;
+      hipError_t e = hipGetDevice(&dev);
+      if (e != hipSuccess) return e;
+      const uint64_t bit = (uint64_t)1 << (dev & 63);
+      if (!(ready.load(std::memory_order_relaxed) & bit) || dev > 63) {
+        e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        ready.fetch_or(bit, std::memory_order_relaxed);
+      }
+      const int tiles = (rows + kWideRows - 1) / kWideRows;
+      hipLaunchKernelGGL((decode_wide_kernel<D, FMT, DT>), dim3((unsigned)(heads * tiles * pl.shared_chunks)),
+                         dim3(kThreads), lds, stream, a, tiles);
+    } else {
+      const int tiles = (rows + 15) / 16;
+      hipLaunchKernelGGL((decode_narrow_kernel<D, FMT, DT, true>), dim3((unsigned)(heads * tiles * pl.shared_chunks)),
+                         dim3(kThreads), 0, stream, a, tiles);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int tiles = (pl.rows + 15) / 16;
+  hipLaunchKernelGGL((decode_narrow_kernel<D, FMT, DT, false>),
+                     dim3((unsigned)((int64_t)heads * tiles * pl.own_chunks * a.batch.batch)), dim3(kThreads), 0, stream,
+                     a, tiles);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || pl.direct) return e;
+  constexpr int slots = kThreads / (D / 4);
+  int split = 1;
+  while (split < slots && 2 * split <= pl.max_parts) split *= 2;
+  const int64_t all_rows = (int64_t)pl.tokens * a.n_q_heads;
+  const int per = slots / split;
+  hipLaunchKernelGGL((decode_merge_kernel<D, DT>), dim3((unsigned)((all_rows + per - 1) / per)), dim3(kThreads), 0,
+                     stream, a, split);
+  return hipGetLastError();
+}
+
+template <int D, int FMT>
+hipError_t launch_dtype(const DecodeAttnArgs &a, hipStream_t stream) {
+  return a.pool.dtype == SC_DTYPE_BF16 ? launch_all<D, FMT, SC_DTYPE_BF16>(a, stream)
+                                       : launch_all<D, FMT, SC_DTYPE_F16>(a, stream);
+}
+template <int D>
+hipError_t launch_format(const DecodeAttnArgs &a, hipStream_t stream) {
+  switch (a.pool.kv_format) {
+    case SC_KV_16BIT: return launch_dtype<D, SC_KV_16BIT>(a, stream);
+    case SC_KV_INT8: return launch_dtype<D, SC_KV_INT8>(a, stream);
+    default: return launch_dtype<D, SC_KV_E4M3>(a, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_decode_attn(const DecodeAttnArgs &a, hipStream_t stream) {
+  return a.pool.head_dim == 128 ? launch_format<128>(a, stream) : launch_format<64>(a, stream);
+}
+
+}  // namespace sc

@@ -37,23 +37,6 @@ sc_status fail_hip(hipError_t e, const char *what) {
 
 void clear_error() { g_last_error.clear(); }
 
-// Makes `dev` current for the duration of a call and restores the caller's.
-class DeviceGuard {
- public:
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&old_) != hipSuccess) old_ = -1;
-    if (old_ != dev) ok_ = hipSetDevice(dev) == hipSuccess;
-  }
-  ~DeviceGuard() {
-    if (old_ >= 0) (void)hipSetDevice(old_);
-  }
-  bool ok() const { return ok_; }
-
- private:
-  int old_ = -1;
-  bool ok_ = true;
-};
-
 // ---------------------------------------------------------------------------
 // Attention planner
 // ---------------------------------------------------------------------------
@@ -1025,8 +1008,8 @@ bool dispatch_is_serialised() {
 // CU that holds an attention workgroup (one wave per SIMD beside the
 // attention's two; 512 VGPRs per SIMD lane, allocated in steps of 8).  Only then may attention wait for the
 // copy stream on the device without risking a wait on itself.
-bool copy_fits_beside_attention(int head_dim) {
-  const int av = attn_fwd_vgprs(head_dim), cv = kv_copy_vgprs();
+bool copy_fits_beside_attention(int head_dim, int kv_format) {
+  const int av = attn_fwd_vgprs(head_dim), cv = std::max(kv_copy_vgprs(), kv_format == SC_KV_16BIT ? 0 : kv8_copy_vgprs(kv_format));
   if (av <= 0 || cv <= 0) return false;
   auto alloc = [](int v) { return (v + 7) / 8 * 8; };
   return 2 * alloc(av) + alloc(cv) <= 512;
@@ -1040,7 +1023,7 @@ bool copy_fits_beside_attention(int head_dim) {
 bool stack_device_wait(const sc_table *t, uint32_t flags) {
   if ((flags & SC_STACK_MODE_MASK) != SC_STACK_OVERLAP) return false;
   if ((flags & SC_STACK_EVENT_WAIT) != 0 || dispatch_is_serialised()) return false;
-  return t->n_fetch_host > 0 || copy_fits_beside_attention(t->pool->desc.head_dim);
+  return t->n_fetch_host > 0 || copy_fits_beside_attention(t->pool->desc.head_dim, t->pool->kv_format);
 }
 
 size_t copy_lds_reserve(int device, int head_dim, bool narrow) {
@@ -1086,7 +1069,7 @@ int copy_groups_beside_attention(int device, const sc_table *t, int n_q_heads, i
   const double flops = 4.0 * head_dim * n_q_heads * pairs;
   int64_t rows = 0;
   for (const CopyItem &it : t->h_items) rows += it.nrows;
-  const double bytes = 2.0 * (double)rows * (double)t->pool->row_bytes;
+  const double bytes = 2.0 * (double)rows * (double)t->pool->act_row_bytes;
   int cus = 0;
   if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess || cus <= 0) return 0;
   if (flops <= 0.0) return 0;
@@ -1098,7 +1081,12 @@ int copy_groups_beside_attention(int device, const sc_table *t, int n_q_heads, i
 CopyArgs copy_args(const sc_pool *p, const sc_table *t, int mode) {
   CopyArgs a{};
   a.mode = mode;
-  a.row_bytes = (int64_t)p->row_bytes;
+  a.row_bytes = (int64_t)(mode == COPY_APPEND ? p->act_row_bytes : p->row_bytes);
+  a.kv_format = p->kv_format;
+  a.dtype = p->desc.dtype;
+  a.n_heads = p->desc.n_kv_heads;
+  a.dim_shift = p->desc.head_dim == 128 ? 7 : 6;
+  a.scale_off = (int64_t)p->scale_off;
   a.v_half_off = (int64_t)(p->slice_bytes / 2);
   a.tier_base[0] = p->dev_base;
   a.tier_base[1] = p->host_dev;
@@ -1337,8 +1325,7 @@ const char *sc_last_error(void) { return g_last_error.c_str(); }
 
 const char *sc_version(void) { return "swiftcache-mi355x 0.1 (gfx950)"; }
 
-sc_status sc_pool_create(const sc_pool_desc *desc, sc_pool **out) {
-  clear_error();
+static sc_status create_pool(const sc_pool_desc *desc, int32_t kv_format, sc_pool **out) {
   if (desc == nullptr || out == nullptr) return fail(SC_ERR_INVALID, "null argument");
   *out = nullptr;
   const sc_pool_desc &d = *desc;
@@ -1347,6 +1334,10 @@ sc_status sc_pool_create(const sc_pool_desc *desc, sc_pool **out) {
       d.n_device_blocks + d.n_host_blocks + d.n_rc_blocks <= 0 ||
       (d.dtype != SC_DTYPE_BF16 && d.dtype != SC_DTYPE_F16))
     return fail(SC_ERR_INVALID, "invalid pool description");
+  if (kv_format != SC_KV_16BIT && kv_format != SC_KV_INT8 && kv_format != SC_KV_E4M3)
+    return fail(SC_ERR_INVALID, "unknown kv_format %d", kv_format);
+  if (kv_format != SC_KV_16BIT && d.n_rc_blocks > 0)
+    return fail(SC_ERR_UNSUPPORTED, "a regular cache holds 16-bit K and V (kv_format %d)", kv_format);
   if (d.head_dim != 64 && d.head_dim != 128)
     return fail(SC_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", d.head_dim);
   // The copy kernels address one block's K (or V) rows of a layer with
@@ -1379,8 +1370,15 @@ sc_status sc_pool_create(const sc_pool_desc *desc, sc_pool **out) {
   std::unique_ptr<sc_pool> p(new sc_pool());
   p->desc = d;
   p->dev_lent = d.n_device_blocks;
-  p->row_bytes = (size_t)d.n_kv_heads * d.head_dim * 2;
-  p->slice_bytes = 2 * (size_t)d.block_size * p->row_bytes;   // Eq. 1 with bf16
+  p->kv_format = kv_format;
+  p->act_row_bytes = (size_t)d.n_kv_heads * d.head_dim * 2;
+  p->row_bytes = kv_format == SC_KV_16BIT ? p->act_row_bytes : p->act_row_bytes / 2;
+  size_t half_bytes = (size_t)d.block_size * p->row_bytes;
+  if (kv_format != SC_KV_16BIT) {
+    p->scale_off = half_bytes;
+    half_bytes = (half_bytes + (size_t)d.block_size * d.n_kv_heads * 2 + 15) & ~(size_t)15;
+  }
+  p->slice_bytes = 2 * half_bytes;   // Eq. 1 with 16-bit elements, or one byte each and the scales
   p->block_bytes = (size_t)d.n_layers * p->slice_bytes;
   const size_t dev_bytes = (size_t)d.n_device_blocks * p->block_bytes;
   const size_t host_bytes = (size_t)d.n_host_blocks * p->block_bytes;
@@ -1440,6 +1438,25 @@ sc_status sc_pool_create(const sc_pool_desc *desc, sc_pool **out) {
     }
   }
   *out = p.release();
+  return SC_OK;
+}
+
+sc_status sc_pool_create(const sc_pool_desc *desc, sc_pool **out) {
+  clear_error();
+  return create_pool(desc, SC_KV_16BIT, out);
+}
+
+sc_status sc_pool_create_quant(const sc_pool_desc *desc, int32_t kv_format, sc_pool **out) {
+  clear_error();
+  return create_pool(desc, kv_format, out);
+}
+
+sc_status sc_pool_quant_get(const sc_pool *pool, int32_t *kv_format, size_t *half_bytes, size_t *scale_offset) {
+  clear_error();
+  if (!pool) return fail(SC_ERR_INVALID, "null pool");
+  if (kv_format) *kv_format = pool->kv_format;
+  if (half_bytes) *half_bytes = pool->slice_bytes / 2;
+  if (scale_offset) *scale_offset = pool->kv_format == SC_KV_16BIT ? pool->slice_bytes / 2 : pool->scale_off;
   return SC_OK;
 }
 
@@ -1628,6 +1645,7 @@ sc_status sc_table_create(sc_pool *pool, int32_t batch, const int32_t *block_ids
       CopyItem it{};
       locate(ids[blk], &it);
       it.pool_off += (pos % bs) * (int64_t)pool->row_bytes;
+      it.act_row = pos % bs;
       it.src_row = t->cu_q[b] + (pos - P);
       it.nrows = (int32_t)(end - pos);
       store.push_back(it);
@@ -1790,6 +1808,8 @@ sc_status sc_fetch_layer_kv_dma(sc_pool *pool, const sc_table *table, int32_t la
   if (table->pool != pool) return fail(SC_ERR_INVALID, "table belongs to another pool");
   if (layer < 0 || layer >= pool->desc.n_layers)
     return fail(SC_ERR_RANGE, "layer %d outside [0, %d)", layer, pool->desc.n_layers);
+  if (pool->kv_format != SC_KV_16BIT)
+    return fail(SC_ERR_UNSUPPORTED, "the copy engines do not convert 8-bit blocks (kv_format %d)", pool->kv_format);
   sc_status st = check_active(table, dst);
   if (st != SC_OK) return st;
   DeviceGuard guard(pool->desc.device);
@@ -2149,7 +2169,7 @@ sc_status prefill_stack(sc_pool *pool, const sc_table *table, int32_t n_layers, 
   }
   // Debug poisoning: NaN patterns over a slot's K and V before it is refilled.
   auto poison_slot = [&](const sc_active &slot, hipStream_t s) -> sc_status {
-    const size_t bytes = (size_t)table->total_kv * pool->row_bytes;
+    const size_t bytes = (size_t)table->total_kv * pool->act_row_bytes;
     const uint16_t nan16 = d.dtype == SC_DTYPE_F16 ? 0x7E00 : 0x7FC0;
     hipError_t e = launch_kv_fill(slot.k, bytes, nan16, s);
     if (e == hipSuccess) e = launch_kv_fill(slot.v, bytes, nan16, s);

@@ -29,6 +29,23 @@ void clear_error();
     if (e_ != hipSuccess) return ::sc::fail_hip(e_, #call); \
   } while (0)
 
+// Makes `dev` current for the duration of a call and restores the caller's.
+class DeviceGuard {
+ public:
+  explicit DeviceGuard(int dev) {
+    if (hipGetDevice(&old_) != hipSuccess) old_ = -1;
+    if (old_ != dev) ok_ = hipSetDevice(dev) == hipSuccess;
+  }
+  ~DeviceGuard() {
+    if (old_ >= 0) (void)hipSetDevice(old_);
+  }
+  bool ok() const { return ok_; }
+
+ private:
+  int old_ = -1;
+  bool ok_ = true;
+};
+
 // ---------------------------------------------------------------------------
 // Copy work items (fetch / append / store).  One item moves `nrows` token
 // rows of K and, in a second workgroup, of V.
@@ -39,7 +56,7 @@ void clear_error();
 // ---------------------------------------------------------------------------
 struct CopyItem {
   int64_t pool_off;   // bytes from the tier base to the first row (layer 0, K half)
-  int64_t act_row;    // first row in the active buffer (FETCH/APPEND)
+  int64_t act_row;    // first row in the active buffer (FETCH/APPEND); STORE: the first row's place in its block
   int64_t src_row;    // first row of k_new / v_new (APPEND/STORE)
   int32_t nrows;
   int32_t tier;       // 0 = device tier, 1 = host tier
@@ -62,6 +79,14 @@ struct CopyArgs {
   const char *new_k;
   const char *new_v;
   int32_t serial_stores;  // set by the launch: one store in flight per wave
+  // Pools of 8-bit blocks (kv_format != SC_KV_16BIT): row_bytes is a token's
+  // codes, a row of the active buffer and of new_k / new_v has 2 * row_bytes,
+  // and the scales of a half start scale_off bytes into it.
+  int32_t kv_format;
+  int32_t dtype;
+  int32_t n_heads;
+  int32_t dim_shift;      // log2(head_dim)
+  int64_t scale_off;
 };
 
 // lds_reserve: bytes of LDS each copy workgroup reserves without using them
@@ -83,6 +108,9 @@ struct LayerCopyArgs {
   uint32_t nan2;                   // nan16 repeated in both halves
 };
 hipError_t launch_kv_layer_copy(const LayerCopyArgs &a, hipStream_t stream, size_t lds_reserve, int max_groups);
+// What this and launch_kv_copy do for pools of 8-bit blocks (kv8_copy.hip).
+hipError_t launch_kv8_copy(const CopyArgs &a, hipStream_t stream, size_t lds_reserve, int max_groups);
+hipError_t launch_kv8_layer_copy(const LayerCopyArgs &a, hipStream_t stream, size_t lds_reserve, int max_groups);
 // One-wave kernel that sets *filled = filled_value, then holds the stream
 // until *counter >= value (the attention workgroups that read a slot are all
 // done with it; value 0: no wait), polling at most spin_limit times; on
@@ -91,6 +119,95 @@ hipError_t launch_kv_layer_copy(const LayerCopyArgs &a, hipStream_t stream, size
 hipError_t launch_slot_gate(uint64_t *filled, uint64_t filled_value, const uint64_t *counter, uint64_t value,
                             uint32_t *timeout, uint64_t *fail_word, uint64_t fail_tag, int spin_limit,
                             hipStream_t stream);
+
+// ---------------------------------------------------------------------------
+// Rotary positions and decode steps (rope.hip, decode_attn.hip)
+// ---------------------------------------------------------------------------
+// What a kernel needs to rotate one head: turns[i] = theta_i / (2 pi).
+struct RopeView {
+  const double *turns;    // nullptr: no rotation
+  int32_t half;           // rotary_dim / 2
+  int32_t interleaved;
+  float amplitude;
+};
+
+struct RopeArgs {
+  RopeView rope;
+  const int32_t *positions;
+  const uint16_t *x[2];   // q, k
+  uint16_t *y[2];
+  int64_t x_stride[2], y_stride[2];   // elements between tokens
+  int32_t heads[2];
+  int32_t n_tokens;
+  int32_t dtype;
+  int32_t dim_shift;
+  int32_t in_place[2];
+};
+hipError_t launch_rope(const RopeArgs &a, hipStream_t stream);
+
+// The pool as the decode kernels see it: block id -> tier, layer slice.
+struct PoolView {
+  char *tier[3];          // HBM, host and regular-cache tiers
+  int64_t first[2];       // first id of the host and of the regular-cache tier
+  int64_t n_ids;          // ids below this exist
+  int64_t lent;           // HBM ids below this are usable
+  int64_t block_bytes;
+  int64_t layer_off;
+  int64_t half_bytes;     // V half after the K half
+  int64_t scale_off;      // 8-bit formats: scales after a half's codes
+  int32_t block_size;
+  uint32_t block_magic;   // t / block_size = (t * block_magic) >> (31 + block_shift), t < 2^31
+  int32_t block_shift;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t kv_format;
+  int32_t dtype;
+};
+
+struct DecodeView {
+  const int32_t *block_ids;
+  const int32_t *kv_len;
+  const int32_t *shared_ids;
+  int32_t batch, n_new, max_blocks, max_len, shared_len;
+};
+
+struct DecodeStoreArgs {
+  PoolView pool;
+  DecodeView batch;
+  RopeView rope;
+  const uint16_t *k, *v, *q;
+  uint16_t *q_out;
+  int32_t n_q_heads;      // 0: no q
+  int32_t q_in_place;
+};
+hipError_t launch_decode_store(const DecodeStoreArgs &a, hipStream_t stream);
+
+// Work of one decode-attention call (see plan_decode).  The key chunks of
+// the shared prefix come first, then those of the sequences' own tokens;
+// partial p of a row is its p-th chunk's.
+struct DecodePlan {
+  int32_t group;              // query heads per KV head
+  int32_t rows;               // rows of one sequence and KV head: n_new * group
+  int32_t tokens;             // batch * n_new
+  int32_t own_chunk, own_chunks;        // keys of a chunk, chunks of max_len (at least one)
+  int32_t shared_chunk, shared_chunks;
+  int32_t shared_wide;        // the shared keys by the kernel for more than 16 rows
+  int32_t direct;             // one chunk and no shared prefix: no partials
+  int32_t max_parts;          // partials of a row: shared_chunks + own_chunks
+};
+struct DecodeAttnArgs {
+  PoolView pool;
+  DecodeView batch;
+  DecodePlan plan;
+  const uint16_t *q;
+  uint16_t *out;
+  float *lse;
+  float *part_o;          // [max_parts][tokens * n_q_heads][head_dim], not divided by the sums
+  float2 *part_ml;        // [max_parts][tokens * n_q_heads]: running maximum (log2 domain) and sum
+  int32_t n_q_heads;
+  float scale_log2;
+};
+hipError_t launch_decode_attn(const DecodeAttnArgs &a, hipStream_t stream);
 
 // ---------------------------------------------------------------------------
 // Attention work decomposition
@@ -237,6 +354,7 @@ int64_t deferred_merge_chunks(int64_t rows, int head_dim, int max_splits);
 size_t attn_fwd_lds_bytes(int head_dim, bool narrow);   // narrow: the kernel for plans with narrow items
 int attn_fwd_vgprs(int head_dim);   // per work item, -1 if unknown
 int kv_copy_vgprs();                // largest of the copy stream's kernels, the slot gate's included
+int kv8_copy_vgprs(int kv_format);  // largest of the kernels that take their place for 8-bit blocks
 hipError_t launch_attn_merge(const AttnArgs &a, int head_dim, int max_splits, hipStream_t stream);
 
 struct AttnPlan {
@@ -300,7 +418,10 @@ struct sc_pool {
   bool own_host = false;
   size_t slice_bytes = 0;
   size_t block_bytes = 0;
-  size_t row_bytes = 0;
+  size_t row_bytes = 0;           // one token of one layer, K or V, in a block
+  int kv_format = SC_KV_16BIT;
+  size_t act_row_bytes = 0;       // ... in an active buffer, k_new and v_new: 16-bit elements
+  size_t scale_off = 0;           // 8-bit formats: scales after the codes of a half
 };
 
 struct sc_table {

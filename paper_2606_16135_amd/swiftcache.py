@@ -30,6 +30,20 @@ SC_DTYPE_BF16 = 0
 SC_DTYPE_F16 = 1
 DTYPE_CODES = {"bf16": SC_DTYPE_BF16, "f16": SC_DTYPE_F16}
 
+SC_KV_16BIT = 0
+SC_KV_INT8 = 1
+SC_KV_E4M3 = 2
+KV_FORMAT_CODES = {"16bit": SC_KV_16BIT, "int8": SC_KV_INT8, "e4m3": SC_KV_E4M3}
+
+SC_ROPE_HALF = 0
+SC_ROPE_INTERLEAVED = 1
+ROPE_LAYOUTS = {"half": SC_ROPE_HALF, "interleaved": SC_ROPE_INTERLEAVED}
+SC_ROPE_PLAIN = 0
+SC_ROPE_LINEAR = 1
+SC_ROPE_BANDED = 2
+SC_ROPE_RAMP = 3
+ROPE_SCALINGS = {"plain": SC_ROPE_PLAIN, "linear": SC_ROPE_LINEAR, "banded": SC_ROPE_BANDED, "ramp": SC_ROPE_RAMP}
+
 SC_STACK_OVERLAP = 0
 SC_STACK_SERIAL = 1
 SC_STACK_ATTN_ONLY = 2
@@ -40,7 +54,7 @@ SC_STACK_TEST_NEVER_FREE = 32
 SC_STACK_EVENT_WAIT = 64
 
 EXPORTED = [
-    "sc_pool_create", "sc_pool_destroy", "sc_pool_layout_get", "sc_table_create",
+    "sc_pool_create", "sc_pool_create_quant", "sc_pool_quant_get", "sc_pool_destroy", "sc_pool_layout_get", "sc_table_create",
     "sc_table_destroy", "sc_table_totals", "sc_table_stack_status", "sc_stack_wait_kind", "sc_fetch_layer_kv",
     "sc_fetch_layer_kv_dma", "sc_append_new_kv",
     "sc_prefill_attn", "sc_prefill_attn_f16", "sc_prefill_attn_noalloc", "sc_attn_noalloc_splits",
@@ -48,6 +62,8 @@ EXPORTED = [
     "sc_prefill_attn_varlen", "sc_store_layer_kv",
     "sc_prefill_stack", "sc_prefill_stack_chunked", "sc_attn_plan_query", "sc_pool_resize", "sc_plan_capacity", "sc_elastic_unit", "sc_scale_up",
     "sc_scale_down", "sc_last_error", "sc_version",
+    "sc_rope_create", "sc_rope_destroy", "sc_rope_frequencies", "sc_rope_apply",
+    "sc_decode_store", "sc_decode_workspace", "sc_decode_attn",
 ]
 
 
@@ -90,6 +106,19 @@ class sc_capacity(ctypes.Structure):
 
 class sc_active(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("capacity_tokens", ctypes.c_int64)]
+
+
+class sc_rope_desc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double),
+                ("amplitude", ctypes.c_double), ("device", ctypes.c_int32)]
+
+
+class sc_decode_batch(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_new", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("block_ids", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("shared_ids", ctypes.c_void_p), ("shared_len", ctypes.c_int32)]
 
 
 _lib = None
@@ -141,6 +170,17 @@ def load():
         "sc_scale_up": (I32, [I64, I32, I64, I64, I64, ctypes.POINTER(I64), ctypes.POINTER(I64)]),
         "sc_scale_down": (I32, [I64, I32, I64, I64, ctypes.POINTER(I64), I32, ctypes.POINTER(I64),
                                 ctypes.POINTER(I64)]),
+        "sc_pool_create_quant": (I32, [ctypes.POINTER(sc_pool_desc), I32, ctypes.POINTER(P)]),
+        "sc_pool_quant_get": (I32, [P, ctypes.POINTER(I32), ctypes.POINTER(ctypes.c_size_t),
+                                    ctypes.POINTER(ctypes.c_size_t)]),
+        "sc_rope_create": (I32, [ctypes.POINTER(sc_rope_desc), ctypes.POINTER(P)]),
+        "sc_rope_destroy": (None, [P]),
+        "sc_rope_frequencies": (I32, [P, ctypes.POINTER(ctypes.c_double), I32, ctypes.POINTER(I32)]),
+        "sc_rope_apply": (I32, [P, I32, I64, VP, VP, I64, I32, VP, I64, VP, I64, I32, VP, I64, VP]),
+        "sc_decode_store": (I32, [P, I32, ctypes.POINTER(sc_decode_batch), VP, VP, P, VP, I32, VP, VP]),
+        "sc_decode_workspace": (I32, [P, ctypes.POINTER(sc_decode_batch), I32, ctypes.POINTER(ctypes.c_size_t)]),
+        "sc_decode_attn": (I32, [P, I32, ctypes.POINTER(sc_decode_batch), VP, I32, F32, VP, VP, VP, ctypes.c_size_t,
+                                 VP]),
         "sc_last_error": (ctypes.c_char_p, []),
         "sc_version": (ctypes.c_char_p, []),
     }
@@ -173,6 +213,22 @@ def sc_pool_create(n_layers, n_kv_heads, head_dim, block_size, n_device_blocks, 
     h = ctypes.c_void_p()
     _check(load().sc_pool_create(ctypes.byref(d), ctypes.byref(h)))
     return h.value
+
+
+def sc_pool_create_quant(kv_format, n_layers, n_kv_heads, head_dim, block_size, n_device_blocks, n_host_blocks=0,
+                         device=0, device_base=0, host_base=0, n_rc_blocks=0, rc_base=0, dtype=SC_DTYPE_BF16):
+    d = sc_pool_desc(n_layers, n_kv_heads, head_dim, block_size, n_device_blocks, n_host_blocks,
+                     device, dtype, device_base or None, host_base or None, n_rc_blocks, rc_base or None)
+    h = ctypes.c_void_p()
+    _check(load().sc_pool_create_quant(ctypes.byref(d), kv_format, ctypes.byref(h)))
+    return h.value
+
+
+def sc_pool_quant_get(pool):
+    """Returns (kv_format, half_bytes, scale_offset)."""
+    fmt, half, off = ctypes.c_int32(), ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load().sc_pool_quant_get(pool, ctypes.byref(fmt), ctypes.byref(half), ctypes.byref(off)))
+    return fmt.value, half.value, off.value
 
 
 def sc_pool_destroy(pool):
@@ -362,3 +418,52 @@ def sc_prefill_stack_chunked(pool, table, q_ptrs, knew_ptrs, vnew_ptrs, out_ptrs
     _check(load().sc_prefill_stack_chunked(pool, table, n, arr(*q_ptrs), arr(*knew_ptrs), arr(*vnew_ptrs),
                                            arr(*out_ptrs), slot_arr, n_q_heads, scale, flags, chunk_tokens,
                                            compute_stream or None, copy_stream or None))
+
+
+def sc_rope_create(head_dim, rotary_dim, layout=SC_ROPE_HALF, base=10000.0, scaling=SC_ROPE_PLAIN, factor=1.0,
+                   original_len=0.0, low=0.0, high=0.0, amplitude=0.0, device=0):
+    d = sc_rope_desc(head_dim, rotary_dim, layout, scaling, base, factor, original_len, low, high, amplitude, device)
+    h = ctypes.c_void_p()
+    _check(load().sc_rope_create(ctypes.byref(d), ctypes.byref(h)))
+    return h.value
+
+
+def sc_rope_destroy(rope):
+    load().sc_rope_destroy(rope)
+
+
+def sc_rope_frequencies(rope):
+    """The scaled frequencies, radians per position."""
+    n = ctypes.c_int32()
+    _check(load().sc_rope_frequencies(rope, None, 0, ctypes.byref(n)))
+    theta = (ctypes.c_double * n.value)()
+    _check(load().sc_rope_frequencies(rope, theta, n.value, ctypes.byref(n)))
+    return list(theta)
+
+
+def sc_rope_apply(rope, dtype, n_tokens, positions, q, q_stride, n_q_heads, q_out, q_out_stride, k, k_stride,
+                  n_kv_heads, k_out, k_out_stride, stream=0):
+    _check(load().sc_rope_apply(rope, dtype, n_tokens, positions or None, q or None, q_stride, n_q_heads,
+                                q_out or None, q_out_stride, k or None, k_stride, n_kv_heads, k_out or None,
+                                k_out_stride, stream or None))
+
+
+def decode_batch(batch, n_new, max_blocks, max_len, block_ids, kv_len, shared_ids=0, shared_len=0):
+    return sc_decode_batch(batch, n_new, max_blocks, max_len, block_ids or None, kv_len or None, shared_ids or None,
+                           shared_len)
+
+
+def sc_decode_store(pool, layer, batch, k_new, v_new, rope=0, q=0, n_q_heads=0, q_out=0, stream=0):
+    _check(load().sc_decode_store(pool, layer, ctypes.byref(batch), k_new or None, v_new or None, rope or None,
+                                  q or None, n_q_heads, q_out or None, stream or None))
+
+
+def sc_decode_workspace(pool, batch, n_q_heads):
+    n = ctypes.c_size_t()
+    _check(load().sc_decode_workspace(pool, ctypes.byref(batch), n_q_heads, ctypes.byref(n)))
+    return n.value
+
+
+def sc_decode_attn(pool, layer, batch, q, n_q_heads, out, workspace=0, workspace_bytes=0, lse=0, scale=0.0, stream=0):
+    _check(load().sc_decode_attn(pool, layer, ctypes.byref(batch), q or None, n_q_heads, scale, out or None,
+                                 lse or None, workspace or None, workspace_bytes, stream or None))
