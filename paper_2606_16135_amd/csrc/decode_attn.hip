@@ -11,7 +11,7 @@
 // largest m, o = sum 2^(m - M) O / sum 2^(m - M) l.  One chunk in all and no
 // shared prefix: the first kernel writes the result itself.
 //
-// decode_narrow_kernel: up to 16 rows of one KV head (the tokens and query
+// Narrow (narrow_body): up to 16 rows of one KV head (the tokens and query
 // heads of one sequence) against one chunk, bound by reading K and V once:
 // 16 rows take the matrix units 16 cycles for 2 KiB (16-bit) that HBM
 // delivers to a CU in 230.  K and V go from memory straight into the operand
@@ -25,10 +25,10 @@
 //       exchange between lanes, and the dims of operand d are D / 16 * m + d:
 //       a lane loads D / 16 contiguous elements of 8 keys and the D / 16
 //       operands are that square transposed in registers.
-// A wave takes 64 keys at a time (up to 32 KiB of loads in flight), the four
-// waves of a workgroup take turns, and join their partials through LDS.
+// A wave takes 16 KiB of K and V at a time, the four waves of a workgroup take
+// turns, and join their partials through LDS.
 //
-// decode_wide_kernel: more rows than that share the keys (a shared prefix:
+// Wide (wide_body): more rows than that share the keys (a shared prefix:
 // every row of the batch).  A workgroup of four waves of 32 rows takes
 // 128-key tiles through LDS: the tile is loaded to registers while the one
 // before is computed, then converted to 16 bits (8-bit codes are exact in
@@ -60,7 +60,6 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
-constexpr int kStep = 64;             // keys of a wave's step (narrow)
 constexpr int kTile = 128;            // keys of a workgroup's tile (wide)
 constexpr int kWideRows = 128;
 constexpr float kNegInf = -__builtin_inff();
@@ -84,6 +83,8 @@ struct Geo {
   static constexpr int kLoads = kRow / 64;               // 16-byte K loads of a lane
   static constexpr int kVd = D / 16;                     // dims a lane takes of a V row
   static constexpr int kVWords = kVd * kElem / 4;        // ... in 32-bit words
+  // Keys of a wave's step (narrow): 16 KiB of K and V, 128 registers of a lane's 256.
+  static constexpr int kStep = kRow == 256 ? 32 : 64;
 };
 
 // First head element of lane group g's slots in MFMA step c.
@@ -220,19 +221,31 @@ __device__ __forceinline__ void store_f32(float *p, const float (&v)[N]) {
 // one KV head, 16 rows.  Blocks are ordered (sequence, chunk, row tile, KV
 // head): the row tiles of a chunk land on one XCD when there are 8 KV heads
 // and read its L2.
+//
+// A wave's step t is pipelined with the next through the registers
+// that it frees: K(t + 1) is loaded once the scores of step t are taken and
+// arrives during their softmax and the PV product, V(t + 1) once that product
+// is done.  Loads return in order, so what a later address needs (the block
+// id, two steps ahead, and the scales) is issued before the K and V loads that
+// it must not wait for.
 // ---------------------------------------------------------------------------
+template <int D>
+struct NarrowLds {
+  uint64_t addr[kWaves][64];
+  float scale[kWaves][2][64];
+  float o[kWaves][16][D];
+  float ml[kWaves][16][2], row[16][2];
+  int bad;
+};
+
 template <int D, int FMT, int DT, bool SHARED>
-__global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnArgs a, int row_tiles) {
+__device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int row_tiles, char *smem) {
   using G = Geo<D, FMT>;
   constexpr int kPv = pv_type<FMT, DT>();
-  __shared__ __attribute__((aligned(16))) uint64_t s_addr[kWaves][kStep];
-  __shared__ __attribute__((aligned(16))) float s_scale[kWaves][2][kStep];
-  __shared__ float s_ml[kWaves][16][2], s_row[16][2];
-  __shared__ __attribute__((aligned(16))) float s_o[kWaves][16][D];
-  __shared__ int s_bad;
+  constexpr int kStep = G::kStep, kTiles = kStep / 16, kHalves = kStep / 32;
+  NarrowLds<D> &lds = *reinterpret_cast<NarrowLds<D> *>(smem);
 
   const PoolView &p = a.pool;
-  int id = blockIdx.x;
   const int kvh = id % p.n_kv_heads;
   id /= p.n_kv_heads;
   const int tile = id % row_tiles;
@@ -260,22 +273,64 @@ __global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnAr
   const int head = kvh * group + (has_row ? row - tok_in * group : 0);
   const int limit = SHARED ? len : len - n_new + tok_in + 1; // keys below it are the row's
 
-  // Q^T operands.
-  u32x4 qf[G::kSteps];
-  const uint16_t *qrow = a.q + ((int64_t)token * a.n_q_heads + head) * D;
-#pragma unroll
-  for (int c = 0; c < G::kSteps; ++c)
-    qf[c] = has_row ? *reinterpret_cast<const u32x4 *>(qrow + slot_dim<D, FMT>(c, g)) : u32x4{0, 0, 0, 0};
-
-  if (threadIdx.x == 0) s_bad = len == kBad ? 1 : 0;
-  __syncthreads();
-
   const int32_t *ids = SHARED ? a.batch.shared_ids : a.batch.block_ids + (int64_t)seq * a.batch.max_blocks;
   const int64_t head_off = (int64_t)kvh * G::kRow;
   const int64_t row_bytes = (int64_t)p.n_kv_heads * G::kRow;
   // Keys from here on are hidden from some row of the tile.
   const int first_tok = tile * 16 / group;
   const int min_limit = SHARED ? len : len - n_new + first_tok + 1;
+  constexpr int kStride = kWaves * kStep;
+
+  if (threadIdx.x == 0) lds.bad = len == kBad ? 1 : 0;
+  __syncthreads();
+
+  uint32_t ks = 0, vs = 0;                   // this lane's key's scales, of the step addressed last
+  // Addresses of the step at `base`, whose lane's block is `blk_id`; false
+  // if an id is outside the pool (nothing of the step is then read).
+  auto take_addr = [&](int base, int32_t blk_id) {
+    const int key = min(base + lane, k1 - 1);
+    const char *blk = block_layer(p, blk_id);
+    if (__any(blk == nullptr)) {
+      lds.bad = 1;
+      return false;
+    }
+    const int in_block = key - block_of(p, key) * p.block_size;
+    if constexpr (G::k8) {
+      const char *sp = blk + p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
+      ks = *reinterpret_cast<const uint16_t *>(sp);
+      vs = *reinterpret_cast<const uint16_t *>(sp + p.half_bytes);
+    }
+    lds.addr[wave][lane] = reinterpret_cast<uint64_t>(blk + in_block * row_bytes + head_off);
+    wave_lds_order();
+    return true;
+  };
+  auto fetch_id = [&](int base) { return ids[block_of(p, min(base + lane, k1 - 1))]; };
+  u32x4 kr[kTiles][G::kLoads];
+  auto load_k = [&] {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const char *kp = reinterpret_cast<const char *>(lds.addr[wave][16 * t + n]) + 16 * g;
+#pragma unroll
+      for (int c = 0; c < G::kLoads; ++c) kr[t][c] = *reinterpret_cast<const u32x4 *>(kp + 64 * c);
+    }
+  };
+  Words<G::kVWords> vr[kHalves][8];
+  auto load_v = [&] {
+#pragma unroll
+    for (int u = 0; u < kHalves; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const char *vp = reinterpret_cast<const char *>(lds.addr[wave][32 * u + 16 * (j >> 2) + 4 * g + (j & 3)]);
+        vr[u][j] = load_words<G::kVWords>(vp + p.half_bytes + n * (G::kVd * G::kElem));
+      }
+  };
+  auto write_scales = [&] {
+    if constexpr (G::k8) {
+      lds.scale[wave][0][lane] = __builtin_bit_cast(float, ks << 16);
+      lds.scale[wave][1][lane] = __builtin_bit_cast(float, vs << 16);
+    }
+    wave_lds_order();
+  };
 
   RowState st = {kNegInf, 0.f};
   f32x4 o[G::kVd];
@@ -283,65 +338,49 @@ __global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnAr
   for (int d = 0; d < G::kVd; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   int base = k0 + wave * kStep;
+  bool more = base < k1;
   int32_t next_id = 0;
-  if (base < k1) next_id = ids[block_of(p, min(base + lane, k1 - 1))];
-  for (; base < k1; base += kWaves * kStep) {
-    const int key = min(base + lane, k1 - 1);
-    const char *blk = block_layer(p, next_id);
-    const int in_block = key - block_of(p, key) * p.block_size;
-    if (base + kWaves * kStep < k1) next_id = ids[block_of(p, min(base + kWaves * kStep + lane, k1 - 1))];
-    if (__any(blk == nullptr)) {             // an id outside the pool: nothing of it is read
-      s_bad = 1;
-      break;
+  u32x4 qf[G::kSteps];                       // Q^T operands
+  if (more) {
+    const int32_t first_id = fetch_id(base);
+    if (base + kStride < k1) next_id = fetch_id(base + kStride);
+    const uint16_t *qrow = a.q + ((int64_t)token * a.n_q_heads + head) * D;
+#pragma unroll
+    for (int c = 0; c < G::kSteps; ++c)
+      qf[c] = has_row ? *reinterpret_cast<const u32x4 *>(qrow + slot_dim<D, FMT>(c, g)) : u32x4{0, 0, 0, 0};
+    more = take_addr(base, first_id);
+    if (more) {
+      load_k();
+      load_v();
+      write_scales();
     }
-    const char *krow = blk + in_block * row_bytes + head_off;
-    uint32_t ks = 0, vs = 0;
-    if constexpr (G::k8) {
-      const char *sp = blk + p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
-      ks = *reinterpret_cast<const uint16_t *>(sp);
-      vs = *reinterpret_cast<const uint16_t *>(sp + p.half_bytes);
-    }
-    s_addr[wave][lane] = reinterpret_cast<uint64_t>(krow);
-    wave_lds_order();
-
-    u32x4 kr[4][G::kLoads];
+  }
+  while (more) {
+    // Scores: lane (n, g) gets keys 16 t + 4 g + i of row n.
+    float x[4 * kTiles];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const char *kp = reinterpret_cast<const char *>(s_addr[wave][16 * t + n]) + 16 * g;
-#pragma unroll
-      for (int c = 0; c < G::kLoads; ++c) kr[t][c] = *reinterpret_cast<const u32x4 *>(kp + 64 * c);
-    }
-    Words<G::kVWords> vr[2][8];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const char *vp = reinterpret_cast<const char *>(s_addr[wave][32 * u + 16 * (j >> 2) + 4 * g + (j & 3)]);
-        vr[u][j] = load_words<G::kVWords>(vp + p.half_bytes + n * (G::kVd * G::kElem));
-      }
-
-    if constexpr (G::k8) {                   // only now: the scales' loads are older than the ones above
-      s_scale[wave][0][lane] = __builtin_bit_cast(float, ks << 16);
-      s_scale[wave][1][lane] = __builtin_bit_cast(float, vs << 16);
-      wave_lds_order();
-    }
-
-    // Scores of 64 keys: lane (n, g) gets keys 16 t + 4 g + i of row n.
-    float x[16];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < kTiles; ++t) {
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < G::kSteps; ++c) s = mfma16<DT>(k_operand<D, FMT, DT>(kr[t], c), qf[c], s);
       f32x4 sc = {1.f, 1.f, 1.f, 1.f};
-      if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&s_scale[wave][0][16 * t + 4 * g]);
+      if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&lds.scale[wave][0][16 * t + 4 * g]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[4 * t + i] = s[i] * (G::k8 ? sc[i] * a.scale_log2 : a.scale_log2);
+    }
+    const int next = base + kStride;
+    bool have_next = next < k1;
+    if (have_next) {
+      have_next = take_addr(next, next_id);
+      if (have_next) {
+        if (next + kStride < k1) next_id = fetch_id(next + kStride);
+        load_k();
+      }
     }
     const bool edge = base + kStep > min(k1, min_limit);   // the same for the whole wave
     if (edge) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+      for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           if (base + 16 * t + 4 * g + i >= min(limit, k1)) x[4 * t + i] = kNegInf;
@@ -352,13 +391,13 @@ __global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnAr
       for (int d = 0; d < G::kVd; ++d) o[d] *= alpha;
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < kHalves; ++u) {
       u32x4 pf;
       float w[8];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         f32x4 sc = {1.f, 1.f, 1.f, 1.f};
-        if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&s_scale[wave][1][32 * u + 16 * h + 4 * g]);
+        if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&lds.scale[wave][1][32 * u + 16 * h + 4 * g]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           w[4 * h + i] = x[8 * u + 4 * h + i];
@@ -400,23 +439,29 @@ __global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnAr
         }
       }
     }
-    wave_lds_order();
+    if (have_next) {
+      load_v();
+      wave_lds_order();
+      write_scales();
+    }
+    base = next;
+    more = have_next;
   }
 
   // Join the four waves.
   st.l += __shfl_xor(st.l, 16);
   st.l += __shfl_xor(st.l, 32);
   if (g == 0) {
-    s_ml[wave][n][0] = st.m;
-    s_ml[wave][n][1] = st.l;
+    lds.ml[wave][n][0] = st.m;
+    lds.ml[wave][n][1] = st.l;
   }
   __syncthreads();
   float m = kNegInf, l = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_ml[w][n][0]);
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds.ml[w][n][0]);
   const float ref = m == kNegInf ? 0.f : m;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) l += s_ml[w][n][1] * __builtin_amdgcn_exp2f(s_ml[w][n][0] - ref);
+  for (int w = 0; w < kWaves; ++w) l += lds.ml[w][n][1] * __builtin_amdgcn_exp2f(lds.ml[w][n][0] - ref);
   const float f = __builtin_amdgcn_exp2f(st.m - ref);
   // o[d][i]: dim G::kVd * (4 g + i) + d of row n.
 #pragma unroll
@@ -424,14 +469,14 @@ __global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnAr
     float v[G::kVd];
 #pragma unroll
     for (int d = 0; d < G::kVd; ++d) v[d] = o[d][i] * f;
-    store_f32(&s_o[wave][n][G::kVd * (4 * g + i)], v);
+    store_f32(&lds.o[wave][n][G::kVd * (4 * g + i)], v);
   }
   if (wave == 0 && g == 0) {
-    s_row[n][0] = m;
-    s_row[n][1] = l;
+    lds.row[n][0] = m;
+    lds.row[n][1] = l;
   }
   __syncthreads();
-  const bool bad = s_bad != 0;
+  const bool bad = lds.bad != 0;
   const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
   const int part = SHARED ? chunk : a.plan.shared_chunks + chunk;
   // Thread: 4 dims of a row; 16 rows x D / 4 threads' worth.
@@ -443,8 +488,8 @@ __global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnAr
     const int64_t out_row = (int64_t)(SHARED ? tk : seq * n_new + tk) * a.n_q_heads + kvh * group + (rr - tk * group);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4 *>(&s_o[w][r][d0]);
-    float rm = s_row[r][0], rl = s_row[r][1];
+    for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4 *>(&lds.o[w][r][d0]);
+    float rm = lds.row[r][0], rl = lds.row[r][1];
     if (bad) rm = rl = __builtin_nanf("");
     if (!direct) {
       *reinterpret_cast<f32x4 *>(a.part_o + ((int64_t)part * all_rows + out_row) * D + d0) = v;
@@ -468,12 +513,11 @@ __global__ __launch_bounds__(kThreads, 2) void decode_narrow_kernel(DecodeAttnAr
 // Wide: one chunk of the shared keys, one KV head, 128 rows of the batch.
 // ---------------------------------------------------------------------------
 template <int D, int FMT, int DT>
-__global__ __launch_bounds__(kThreads, 2) void decode_wide_kernel(DecodeAttnArgs a, int row_tiles) {
+__device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int row_tiles, char *smem) {
   using G = Geo<D, FMT>;
   constexpr int kPv = pv_type<FMT, DT>();
   constexpr int kKPer = kTile * G::kRow / 16 / kThreads;      // 16-byte K pieces of a thread
   constexpr int kPieces = G::kRow / 16;                       // ... of a key
-  extern __shared__ __attribute__((aligned(16))) char smem[];
   u32x4 *const s_k = reinterpret_cast<u32x4 *>(smem);         // [8][D / 32][64] operands
   u32x4 *const s_v = s_k + kTile * D / 8;                     // [4][D / 16][64]
   uint64_t(*const s_addr)[kTile] = reinterpret_cast<uint64_t(*)[kTile]>(s_v + kTile * D / 8);   // [2]
@@ -481,7 +525,6 @@ __global__ __launch_bounds__(kThreads, 2) void decode_wide_kernel(DecodeAttnArgs
   int *const s_bad = reinterpret_cast<int *>(s_scale + 2);   // [2], tiles of one parity: set while the other is read
 
   const PoolView &p = a.pool;
-  int id = blockIdx.x;
   const int kvh = id % p.n_kv_heads;
   id /= p.n_kv_heads;
   const int tile = id % row_tiles;
@@ -702,6 +745,22 @@ constexpr size_t wide_lds_bytes() {
   return 2 * (size_t)kTile * D * 2 + 2 * kTile * sizeof(uint64_t) + 2 * kTile * sizeof(float) + 16;
 }
 
+// One launch for both key lists, the shared one's workgroups first: they are
+// the longer ones, and the own keys' loads fill the memory's time beside the
+// wide kernel's matrix work.  WIDE: the shared keys have more than 16 rows.
+template <int D, int FMT, int DT, bool WIDE>
+__global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(DecodeAttnArgs a, int shared_groups, int shared_tiles,
+                                                                  int own_tiles) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int id = blockIdx.x;
+  if (id >= shared_groups)
+    narrow_body<D, FMT, DT, false>(a, id - shared_groups, own_tiles, smem);
+  else if constexpr (WIDE)
+    wide_body<D, FMT, DT>(a, id, shared_tiles, smem);
+  else
+    narrow_body<D, FMT, DT, true>(a, id, shared_tiles, smem);
+}
+
 // ---------------------------------------------------------------------------
 // Merge.  D / 4 lanes hold a row's output, 4 dims each; `split` such lane
 // groups of a workgroup share one row's partials.
@@ -778,41 +837,40 @@ __global__ __launch_bounds__(kThreads) void decode_merge_kernel(DecodeAttnArgs a
     a.lse[(int64_t)head * a.plan.tokens + token] = none ? kNegInf : (m + __builtin_log2f(l)) * 0.6931471805599453f;
 }
 
+template <int D, int FMT, int DT, bool WIDE>
+hipError_t launch_chunks(const DecodeAttnArgs &a, hipStream_t stream) {
+  const DecodePlan &pl = a.plan;
+  constexpr size_t lds = WIDE ? wide_lds_bytes<D>() : sizeof(NarrowLds<D>);
+  static_assert(lds >= sizeof(NarrowLds<D>), "both bodies' LDS");
+  const void *kernel = reinterpret_cast<const void *>(&decode_attn_kernel<D, FMT, DT, WIDE>);
+  if (lds > 64 * 1024) {
+    static std::atomic<uint64_t> ready{0};   // devices on which the kernel may use that much LDS
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = (uint64_t)1 << (dev & 63);
+    if (!(ready.load(std::memory_order_relaxed) & bit) || dev > 63) {
+      e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+      ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+  }
+  const int heads = a.pool.n_kv_heads;
+  const int shared_rows = WIDE ? kWideRows : 16;
+  const int shared_tiles = (pl.tokens * pl.group + shared_rows - 1) / shared_rows;
+  const int own_tiles = (pl.rows + 15) / 16;
+  const int shared_groups = heads * shared_tiles * pl.shared_chunks;
+  const int64_t groups = shared_groups + (int64_t)heads * own_tiles * pl.own_chunks * a.batch.batch;
+  hipLaunchKernelGGL((decode_attn_kernel<D, FMT, DT, WIDE>), dim3((unsigned)groups), dim3(kThreads), lds, stream, a,
+                     shared_groups, shared_tiles, own_tiles);
+  return hipGetLastError();
+}
+
 template <int D, int FMT, int DT>
 hipError_t launch_all(const DecodeAttnArgs &a, hipStream_t stream) {
   const DecodePlan &pl = a.plan;
-  const int heads = a.pool.n_kv_heads;
-  if (pl.shared_chunks > 0) {
-    const int rows = pl.tokens * pl.group;
-    if (pl.shared_wide) {
-      constexpr size_t lds = wide_lds_bytes<D>();
-      const void *kernel = reinterpret_cast<const void *>(&decode_wide_kernel<D, FMT, DT>);
-      static std::atomic<uint64_t> ready{0};   // devices on which the kernel may use that much LDS
-      int dev = 0;
-      hipError_t e = hipGetDevice(&dev);
-      if (e != hipSuccess) return e;
-      const uint64_t bit = (uint64_t)1 << (dev & 63);
-      if (!(ready.load(std::memory_order_relaxed) & bit) || dev > 63) {
-        e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) return e;
-        ready.fetch_or(bit, std::memory_order_relaxed);
-      }
-      const int tiles = (rows + kWideRows - 1) / kWideRows;
-      hipLaunchKernelGGL((decode_wide_kernel<D, FMT, DT>), dim3((unsigned)(heads * tiles * pl.shared_chunks)),
-                         dim3(kThreads), lds, stream, a, tiles);
-    } else {
-      const int tiles = (rows + 15) / 16;
-      hipLaunchKernelGGL((decode_narrow_kernel<D, FMT, DT, true>), dim3((unsigned)(heads * tiles * pl.shared_chunks)),
-                         dim3(kThreads), 0, stream, a, tiles);
-    }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  const int tiles = (pl.rows + 15) / 16;
-  hipLaunchKernelGGL((decode_narrow_kernel<D, FMT, DT, false>),
-                     dim3((unsigned)((int64_t)heads * tiles * pl.own_chunks * a.batch.batch)), dim3(kThreads), 0, stream,
-                     a, tiles);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = pl.shared_wide && pl.shared_chunks > 0 ? launch_chunks<D, FMT, DT, true>(a, stream)
+                                                              : launch_chunks<D, FMT, DT, false>(a, stream);
   if (e != hipSuccess || pl.direct) return e;
   constexpr int slots = kThreads / (D / 4);
   int split = 1;
