@@ -50,6 +50,7 @@
 #include "sc_quant.h"
 
 #include <atomic>
+#include <type_traits>
 
 namespace sc {
 namespace {
@@ -93,20 +94,28 @@ __device__ __forceinline__ int slot_dim(int c, int g) {
   return Geo<D, FMT>::k8 ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
 }
 
+// Loads from an address that was computed, which the compiler cannot see to
+// be global memory: as flat loads they would also count against, and wait
+// for, the LDS accesses between them.
+template <class T>
+__device__ __forceinline__ T load_global(uint64_t at) {
+  return *(const __attribute__((address_space(1))) T *)at;
+}
+
 template <int N>
 struct Words {
   uint32_t w[N];
 };
 template <int N>
-__device__ __forceinline__ Words<N> load_words(const char *p) {
+__device__ __forceinline__ Words<N> load_words(uint64_t at) {
   Words<N> r;
   if constexpr (N == 1) {
-    r.w[0] = *reinterpret_cast<const uint32_t *>(p);
+    r.w[0] = load_global<uint32_t>(at);
   } else if constexpr (N == 2) {
-    const u32x2 v = *reinterpret_cast<const u32x2 *>(p);
+    const u32x2 v = load_global<u32x2>(at);
     r.w[0] = v.x, r.w[1] = v.y;
   } else {
-    const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
+    const u32x4 v = load_global<u32x4>(at);
     r.w[0] = v.x, r.w[1] = v.y, r.w[2] = v.z, r.w[3] = v.w;
   }
   return r;
@@ -171,6 +180,10 @@ __device__ __forceinline__ int own_len(const DecodeAttnArgs &a, int b) {
   if (len < 0) return -1;
   return len > a.batch.max_len || len > (int64_t)a.batch.max_blocks * a.pool.block_size ? kBad : len;
 }
+
+// Whether any lane of the wave says so, as a value the compiler knows to be
+// the wave's own: a branch on it then stays a scalar branch.
+__device__ __forceinline__ bool wave_any(bool x) { return __builtin_amdgcn_ballot_w64(x) != 0; }
 
 // LDS that only one wave uses: its accesses are executed in order, so only
 // the compiler has to keep them so.
@@ -263,7 +276,8 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
   const bool direct = a.plan.direct != 0;
   if (k0 >= k1 && !direct) return;           // the merge counts the chunks that hold keys
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // In a scalar register, and with it every condition that only the wave decides.
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int rows = SHARED ? a.plan.tokens * group : n_new * group;
   const int row = tile * 16 + n;             // this lane's column
@@ -285,33 +299,39 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
   __syncthreads();
 
   uint32_t ks = 0, vs = 0;                   // this lane's key's scales, of the step addressed last
-  // Addresses of the step at `base`, whose lane's block is `blk_id`; false
-  // if an id is outside the pool (nothing of the step is then read).
+  uint64_t key_at = 0, scale_at = 0;         // addresses of its K row and K scale
+  // Addresses of the step at `base`, whose lane's block is `blk_id`.  False
+  // if an id is outside the pool: the addresses of the step before then stay
+  // (with no branch around the loads) and the sequence's rows come out NaN.
   auto take_addr = [&](int base, int32_t blk_id) {
     const int key = min(base + lane, k1 - 1);
     const char *blk = block_layer(p, blk_id);
-    if (__any(blk == nullptr)) {
-      lds.bad = 1;
-      return false;
-    }
+    const bool ok = !wave_any(blk == nullptr);
+    if (!ok) lds.bad = 1;
     const int in_block = key - block_of(p, key) * p.block_size;
     if constexpr (G::k8) {
-      const char *sp = blk + p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
-      ks = *reinterpret_cast<const uint16_t *>(sp);
-      vs = *reinterpret_cast<const uint16_t *>(sp + p.half_bytes);
+      const int64_t off = p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
+      scale_at = ok ? reinterpret_cast<uint64_t>(blk) + off : scale_at;
     }
-    lds.addr[wave][lane] = reinterpret_cast<uint64_t>(blk + in_block * row_bytes + head_off);
+    key_at = ok ? reinterpret_cast<uint64_t>(blk) + in_block * row_bytes + head_off : key_at;
+    lds.addr[wave][lane] = key_at;
     wave_lds_order();
-    return true;
+    return ok;
+  };
+  auto load_scales = [&] {
+    if constexpr (G::k8) {
+      ks = load_global<uint16_t>(scale_at);
+      vs = load_global<uint16_t>(scale_at + p.half_bytes);
+    }
   };
   auto fetch_id = [&](int base) { return ids[block_of(p, min(base + lane, k1 - 1))]; };
   u32x4 kr[kTiles][G::kLoads];
   auto load_k = [&] {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const char *kp = reinterpret_cast<const char *>(lds.addr[wave][16 * t + n]) + 16 * g;
+      const uint64_t kp = lds.addr[wave][16 * t + n] + 16 * g;
 #pragma unroll
-      for (int c = 0; c < G::kLoads; ++c) kr[t][c] = *reinterpret_cast<const u32x4 *>(kp + 64 * c);
+      for (int c = 0; c < G::kLoads; ++c) kr[t][c] = load_global<u32x4>(kp + 64 * c);
     }
   };
   Words<G::kVWords> vr[kHalves][8];
@@ -320,7 +340,7 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
     for (int u = 0; u < kHalves; ++u)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const char *vp = reinterpret_cast<const char *>(lds.addr[wave][32 * u + 16 * (j >> 2) + 4 * g + (j & 3)]);
+        const uint64_t vp = lds.addr[wave][32 * u + 16 * (j >> 2) + 4 * g + (j & 3)];
         vr[u][j] = load_words<G::kVWords>(vp + p.half_bytes + n * (G::kVd * G::kElem));
       }
   };
@@ -339,7 +359,7 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
 
   int base = k0 + wave * kStep;
   bool more = base < k1;
-  int32_t next_id = 0;
+  int32_t next_id = 0;                       // block of this lane's key of the step after next
   u32x4 qf[G::kSteps];                       // Q^T operands
   if (more) {
     const int32_t first_id = fetch_id(base);
@@ -350,12 +370,15 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
       qf[c] = has_row ? *reinterpret_cast<const u32x4 *>(qrow + slot_dim<D, FMT>(c, g)) : u32x4{0, 0, 0, 0};
     more = take_addr(base, first_id);
     if (more) {
+      load_scales();
       load_k();
       load_v();
       write_scales();
     }
   }
-  while (more) {
+  // One step; AHEAD: another one follows.
+  auto step = [&](auto ahead) {
+    constexpr bool kAhead = decltype(ahead)::value;
     // Scores: lane (n, g) gets keys 16 t + 4 g + i of row n.
     float x[4 * kTiles];
 #pragma unroll
@@ -369,13 +392,11 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
       for (int i = 0; i < 4; ++i) x[4 * t + i] = s[i] * (G::k8 ? sc[i] * a.scale_log2 : a.scale_log2);
     }
     const int next = base + kStride;
-    bool have_next = next < k1;
-    if (have_next) {
-      have_next = take_addr(next, next_id);
-      if (have_next) {
-        if (next + kStride < k1) next_id = fetch_id(next + kStride);
-        load_k();
-      }
+    if constexpr (kAhead) {
+      (void)take_addr(next, next_id);
+      load_scales();
+      next_id = fetch_id(next + kStride);
+      load_k();
     }
     const bool edge = base + kStep > min(k1, min_limit);   // the same for the whole wave
     if (edge) {
@@ -386,7 +407,7 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
           if (base + 16 * t + 4 * g + i >= min(limit, k1)) x[4 * t + i] = kNegInf;
     }
     const float alpha = softmax_step(x, st);
-    if (__any(alpha != 1.f)) {
+    if (wave_any(alpha != 1.f)) {
 #pragma unroll
       for (int d = 0; d < G::kVd; ++d) o[d] *= alpha;
     }
@@ -439,13 +460,19 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
         }
       }
     }
-    if (have_next) {
+    if constexpr (kAhead) {
       load_v();
       wave_lds_order();
       write_scales();
+      base = next;
     }
-    base = next;
-    more = have_next;
+  };
+  // The last step is a copy of its own: a condition around the loads would
+  // join ways with and without them at the loop's top, where the compiler
+  // would then wait for every load instead of K's.
+  if (more) {
+    while (base + kStride < k1) step(std::true_type());
+    step(std::false_type());
   }
 
   // Join the four waves.
@@ -534,7 +561,7 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   const int k1 = min(a.batch.shared_len, k0 + a.plan.shared_chunk);
   const int tiles = (k1 - k0 + kTile - 1) / kTile;
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int rows = a.plan.tokens * group;
   const int row0 = tile * kWideRows + wave * 32;
@@ -581,15 +608,13 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
 #pragma unroll
     for (int i = 0; i < kKPer; ++i) {
       const int idx = tid + kThreads * i;
-      kr[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const char *>(s_addr[t & 1][idx / kPieces]) +
-                                               16 * (idx % kPieces));
+      kr[i] = load_global<u32x4>(s_addr[t & 1][idx / kPieces] + 16 * (idx % kPieces));
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      vr[j] = load_words<G::kVWords>(
-          reinterpret_cast<const char *>(s_addr[t & 1][32 * wave + 16 * (j >> 2) + 4 * g + (j & 3)]) + p.half_bytes +
-          n * (G::kVd * G::kElem));
-    if constexpr (G::k8) scale_bits = *reinterpret_cast<const uint16_t *>(my_scale);
+      vr[j] = load_words<G::kVWords>(s_addr[t & 1][32 * wave + 16 * (j >> 2) + 4 * g + (j & 3)] + p.half_bytes +
+                                     n * (G::kVd * G::kElem));
+    if constexpr (G::k8) scale_bits = load_global<uint16_t>(reinterpret_cast<uint64_t>(my_scale));
   };
   // Position of lane (m, g)'s K operand of step c: rotated among the 16 keys
   // so that the pieces of one key, which consecutive threads write, fall on
@@ -685,7 +710,7 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const float alpha = softmax_step(x[r], st[r]);
-          if (__any(alpha != 1.f)) {
+          if (wave_any(alpha != 1.f)) {
 #pragma unroll
             for (int d = 0; d < G::kVd; ++d) o[r][d] *= alpha;
           }
