@@ -619,7 +619,8 @@ typedef struct {
  * Two tokens of one call must not name the same row of the same block.
  * Errors: SC_ERR_INVALID (null, misaligned, sizes outside their ranges, rope
  * of another device, q without rope), SC_ERR_UNSUPPORTED (rope of another
- * head_dim), SC_ERR_RANGE (layer; batch * n_new * heads beyond 2^31 - 1).
+ * head_dim), SC_ERR_RANGE (layer; more than 65536 sequences, too many
+ * heads).
  */
 sc_status sc_decode_store(sc_pool *pool, int32_t layer, const sc_decode_batch *batch, const void *k_new,
                           const void *v_new, const sc_rope *rope, const void *q, int32_t n_q_heads, void *q_out,
@@ -648,8 +649,8 @@ sc_status sc_decode_workspace(const sc_pool *pool, const sc_decode_batch *batch,
  * that may overlap, and captured graphs, need workspaces of their own.
  * Errors: SC_ERR_INVALID (null, misaligned, sizes outside their ranges, a
  * workspace too small), SC_ERR_UNSUPPORTED (GQA group > 16), SC_ERR_RANGE
- * (layer; batch * n_new * n_q_heads beyond 2^31 - 1, or more than 2^31 - 257
- * shared or own tokens).
+ * (layer; more than 65536 sequences, 2^31 - 1 rows, 2^31 - 257 shared or own
+ * tokens, or 2^30 steps of 64 or 32 keys over all sequences at max_len).
  */
 sc_status sc_decode_attn(sc_pool *pool, int32_t layer, const sc_decode_batch *batch, const void *q,
                          int32_t n_q_heads, float scale, void *out, float *lse, void *workspace,

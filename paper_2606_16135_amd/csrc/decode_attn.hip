@@ -25,8 +25,7 @@
 //       exchange between lanes, and the dims of operand d are D / 16 * m + d:
 //       a lane loads D / 16 contiguous elements of 8 keys and the D / 16
 //       operands are that square transposed in registers.
-// A wave takes 16 KiB of K and V at a time, the four waves of a workgroup take
-// turns, and join their partials through LDS.
+// A wave takes 16 KiB of K and V at a time.
 //
 // Wide (wide_body): more rows than that share the keys (a shared prefix:
 // every row of the batch).  A workgroup of four waves of 32 rows takes
@@ -49,6 +48,7 @@
 #include "sc_pool_view.h"
 #include "sc_quant.h"
 
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -63,6 +63,7 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kTile = 128;            // keys of a workgroup's tile (wide)
 constexpr int kWideRows = 128;
+constexpr int kMergeThreads = 1024;   // at most
 constexpr float kNegInf = -__builtin_inff();
 
 template <int DT>
@@ -85,7 +86,7 @@ struct Geo {
   static constexpr int kVd = D / 16;                     // dims a lane takes of a V row
   static constexpr int kVWords = kVd * kElem / 4;        // ... in 32-bit words
   // Keys of a wave's step (narrow): 16 KiB of K and V, 128 registers of a lane's 256.
-  static constexpr int kStep = kRow == 256 ? 32 : 64;
+  static constexpr int kStep = decode_step_keys(D, FMT);
 };
 
 // First head element of lane group g's slots in MFMA step c.
@@ -119,6 +120,14 @@ __device__ __forceinline__ Words<N> load_words(uint64_t at) {
     r.w[0] = v.x, r.w[1] = v.y, r.w[2] = v.z, r.w[3] = v.w;
   }
   return r;
+}
+
+template <int N>
+__device__ __forceinline__ void store_words(uint16_t *p, const Words<N> &w) {
+  if constexpr (N == 2)
+    *reinterpret_cast<u32x2 *>(p) = u32x2{w.w[0], w.w[1]};
+  else
+    *reinterpret_cast<u32x4 *>(p) = u32x4{w.w[0], w.w[1], w.w[2], w.w[3]};
 }
 
 // K operands of one key: D / 32 steps from its loads.
@@ -230,10 +239,13 @@ __device__ __forceinline__ void store_f32(float *p, const float (&v)[N]) {
 }
 
 // ---------------------------------------------------------------------------
-// Narrow: one chunk of one sequence's own keys (SHARED: of the shared ones),
-// one KV head, 16 rows.  Blocks are ordered (sequence, chunk, row tile, KV
-// head): the row tiles of a chunk land on one XCD when there are 8 KV heads
-// and read its L2.
+// Narrow: a wave takes one chunk of one sequence's own keys (SHARED: of the
+// shared ones), one KV head, 16 rows, and writes a partial of its own; the
+// waves of a workgroup do not meet.  Consecutive waves take the KV heads of
+// one chunk, so that together they read whole token rows: with a workgroup
+// per head, the heads' reads of a row came from eight XCDs at different
+// times, and HBM delivered 5.4 TB/s instead of 5.8 (int8 rows of 128 bytes a
+// head), and the scales of a row were fetched once per XCD.
 //
 // A wave's step t is pipelined with the next through the registers
 // that it frees: K(t + 1) is loaded once the scores of step t are taken and
@@ -242,42 +254,22 @@ __device__ __forceinline__ void store_f32(float *p, const float (&v)[N]) {
 // id, two steps ahead, and the scales) is issued before the K and V loads that
 // it must not wait for.
 // ---------------------------------------------------------------------------
-template <int D>
-struct NarrowLds {
-  uint64_t addr[kWaves][64];
-  float scale[kWaves][2][64];
-  float o[kWaves][16][D];
-  float ml[kWaves][16][2], row[16][2];
-  int bad;
+struct NarrowLds {                           // of one wave
+  uint64_t addr[64];
+  float scale[2][64];
 };
 
+// Keys [k0, k1) of sequence `seq`, as partial `part` of its rows.
 template <int D, int FMT, int DT, bool SHARED>
-__device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int row_tiles, char *smem) {
+__device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, int len, int k0, int k1, int kvh, int tile,
+                                            int64_t part, NarrowLds &lds) {
   using G = Geo<D, FMT>;
   constexpr int kPv = pv_type<FMT, DT>();
   constexpr int kStep = G::kStep, kTiles = kStep / 16, kHalves = kStep / 32;
-  NarrowLds<D> &lds = *reinterpret_cast<NarrowLds<D> *>(smem);
-
   const PoolView &p = a.pool;
-  const int kvh = id % p.n_kv_heads;
-  id /= p.n_kv_heads;
-  const int tile = id % row_tiles;
-  id /= row_tiles;
-  const int n_chunks = SHARED ? a.plan.shared_chunks : a.plan.own_chunks;
-  const int chunk = id % n_chunks;
-  const int seq = SHARED ? 0 : id / n_chunks;
-
+  const int lane = threadIdx.x & 63;
   const int group = a.plan.group;
   const int n_new = a.batch.n_new;
-  const int len = SHARED ? a.batch.shared_len : own_len(a, seq);
-  const int size = SHARED ? a.plan.shared_chunk : a.plan.own_chunk;
-  const int k0 = chunk * size;
-  const int k1 = min(len, k0 + size);
-  const bool direct = a.plan.direct != 0;
-  if (k0 >= k1 && !direct) return;           // the merge counts the chunks that hold keys
-
-  // In a scalar register, and with it every condition that only the wave decides.
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int rows = SHARED ? a.plan.tokens * group : n_new * group;
   const int row = tile * 16 + n;             // this lane's column
@@ -293,10 +285,7 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
   // Keys from here on are hidden from some row of the tile.
   const int first_tok = tile * 16 / group;
   const int min_limit = SHARED ? len : len - n_new + first_tok + 1;
-  constexpr int kStride = kWaves * kStep;
-
-  if (threadIdx.x == 0) lds.bad = len == kBad ? 1 : 0;
-  __syncthreads();
+  bool bad = len == kBad;                    // the rows come out NaN
 
   uint32_t ks = 0, vs = 0;                   // this lane's key's scales, of the step addressed last
   uint64_t key_at = 0, scale_at = 0;         // addresses of its K row and K scale
@@ -307,14 +296,14 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
     const int key = min(base + lane, k1 - 1);
     const char *blk = block_layer(p, blk_id);
     const bool ok = !wave_any(blk == nullptr);
-    if (!ok) lds.bad = 1;
+    bad = bad || !ok;
     const int in_block = key - block_of(p, key) * p.block_size;
     if constexpr (G::k8) {
       const int64_t off = p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
       scale_at = ok ? reinterpret_cast<uint64_t>(blk) + off : scale_at;
     }
     key_at = ok ? reinterpret_cast<uint64_t>(blk) + in_block * row_bytes + head_off : key_at;
-    lds.addr[wave][lane] = key_at;
+    lds.addr[lane] = key_at;
     wave_lds_order();
     return ok;
   };
@@ -329,7 +318,7 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
   auto load_k = [&] {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const uint64_t kp = lds.addr[wave][16 * t + n] + 16 * g;
+      const uint64_t kp = lds.addr[16 * t + n] + 16 * g;
 #pragma unroll
       for (int c = 0; c < G::kLoads; ++c) kr[t][c] = load_global<u32x4>(kp + 64 * c);
     }
@@ -340,14 +329,14 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
     for (int u = 0; u < kHalves; ++u)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint64_t vp = lds.addr[wave][32 * u + 16 * (j >> 2) + 4 * g + (j & 3)];
+        const uint64_t vp = lds.addr[32 * u + 16 * (j >> 2) + 4 * g + (j & 3)];
         vr[u][j] = load_words<G::kVWords>(vp + p.half_bytes + n * (G::kVd * G::kElem));
       }
   };
   auto write_scales = [&] {
     if constexpr (G::k8) {
-      lds.scale[wave][0][lane] = __builtin_bit_cast(float, ks << 16);
-      lds.scale[wave][1][lane] = __builtin_bit_cast(float, vs << 16);
+      lds.scale[0][lane] = __builtin_bit_cast(float, ks << 16);
+      lds.scale[1][lane] = __builtin_bit_cast(float, vs << 16);
     }
     wave_lds_order();
   };
@@ -357,13 +346,13 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
 #pragma unroll
   for (int d = 0; d < G::kVd; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  int base = k0 + wave * kStep;
+  int base = k0;
   bool more = base < k1;
   int32_t next_id = 0;                       // block of this lane's key of the step after next
   u32x4 qf[G::kSteps];                       // Q^T operands
   if (more) {
     const int32_t first_id = fetch_id(base);
-    if (base + kStride < k1) next_id = fetch_id(base + kStride);
+    if (base + kStep < k1) next_id = fetch_id(base + kStep);
     const uint16_t *qrow = a.q + ((int64_t)token * a.n_q_heads + head) * D;
 #pragma unroll
     for (int c = 0; c < G::kSteps; ++c)
@@ -387,15 +376,15 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
 #pragma unroll
       for (int c = 0; c < G::kSteps; ++c) s = mfma16<DT>(k_operand<D, FMT, DT>(kr[t], c), qf[c], s);
       f32x4 sc = {1.f, 1.f, 1.f, 1.f};
-      if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&lds.scale[wave][0][16 * t + 4 * g]);
+      if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&lds.scale[0][16 * t + 4 * g]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[4 * t + i] = s[i] * (G::k8 ? sc[i] * a.scale_log2 : a.scale_log2);
     }
-    const int next = base + kStride;
+    const int next = base + kStep;
     if constexpr (kAhead) {
       (void)take_addr(next, next_id);
       load_scales();
-      next_id = fetch_id(next + kStride);
+      next_id = fetch_id(next + kStep);
       load_k();
     }
     const bool edge = base + kStep > min(k1, min_limit);   // the same for the whole wave
@@ -418,7 +407,7 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         f32x4 sc = {1.f, 1.f, 1.f, 1.f};
-        if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&lds.scale[wave][1][32 * u + 16 * h + 4 * g]);
+        if constexpr (G::k8) sc = *reinterpret_cast<const f32x4 *>(&lds.scale[1][32 * u + 16 * h + 4 * g]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           w[4 * h + i] = x[8 * u + 4 * h + i];
@@ -471,67 +460,115 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int id, int
   // join ways with and without them at the loop's top, where the compiler
   // would then wait for every load instead of K's.
   if (more) {
-    while (base + kStride < k1) step(std::true_type());
+    while (base + kStep < k1) step(std::true_type());
     step(std::false_type());
   }
 
-  // Join the four waves.
   st.l += __shfl_xor(st.l, 16);
   st.l += __shfl_xor(st.l, 32);
-  if (g == 0) {
-    lds.ml[wave][n][0] = st.m;
-    lds.ml[wave][n][1] = st.l;
-  }
-  __syncthreads();
-  float m = kNegInf, l = 0.f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, lds.ml[w][n][0]);
-  const float ref = m == kNegInf ? 0.f : m;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) l += lds.ml[w][n][1] * __builtin_amdgcn_exp2f(lds.ml[w][n][0] - ref);
-  const float f = __builtin_amdgcn_exp2f(st.m - ref);
+  if (!has_row) return;
+  if (bad) st.m = st.l = __builtin_nanf("");
   // o[d][i]: dim G::kVd * (4 g + i) + d of row n.
+  if (SHARED || !a.plan.direct) {
+    // `part` is the partial's first row; rows follow tokens, then heads.
+    const int64_t at = part + (int64_t)(SHARED ? token : tok_in) * a.n_q_heads + head;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v[G::kVd];
+#pragma unroll
+      for (int d = 0; d < G::kVd; ++d) v[d] = o[d][i];
+      store_f32(a.part_o + at * D + G::kVd * (4 * g + i), v);
+    }
+    if (g == 0) a.part_ml[at] = float2{st.m, st.l};
+    return;
+  }
+  const int64_t out_row = (int64_t)token * a.n_q_heads + head;
+  const bool none = !bad && limit <= 0;      // no key at all: zeros
+  const float inv = none ? 0.f : 1.f / st.l;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float v[G::kVd];
+    Words<G::kVd / 2> w;
 #pragma unroll
-    for (int d = 0; d < G::kVd; ++d) v[d] = o[d][i] * f;
-    store_f32(&lds.o[wave][n][G::kVd * (4 * g + i)], v);
+    for (int d = 0; d < G::kVd; d += 2) w.w[d / 2] = none ? 0u : pack16<DT>(o[d][i] * inv, o[d + 1][i] * inv);
+    store_words(a.out + out_row * D + G::kVd * (4 * g + i), w);
   }
-  if (wave == 0 && g == 0) {
-    lds.row[n][0] = m;
-    lds.row[n][1] = l;
-  }
-  __syncthreads();
-  const bool bad = lds.bad != 0;
-  const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
-  const int part = SHARED ? chunk : a.plan.shared_chunks + chunk;
-  // Thread: 4 dims of a row; 16 rows x D / 4 threads' worth.
-  for (int idx = threadIdx.x; idx < 16 * (D / 4); idx += kThreads) {
-    const int r = idx / (D / 4), d0 = 4 * (idx % (D / 4));
-    const int rr = tile * 16 + r;
-    if (rr >= rows) continue;
-    const int tk = rr / group;
-    const int64_t out_row = (int64_t)(SHARED ? tk : seq * n_new + tk) * a.n_q_heads + kvh * group + (rr - tk * group);
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (g == 0 && a.lse != nullptr)
+    a.lse[(int64_t)head * a.plan.tokens + token] = none ? kNegInf : (st.m + __builtin_log2f(st.l)) * 0.6931471805599453f;
+}
+
+// Steps of a sequence's own keys.
+template <int D, int FMT>
+__device__ __forceinline__ int steps_of(int len) {
+  return len > 0 ? (len + Geo<D, FMT>::kStep - 1) / Geo<D, FMT>::kStep : 0;
+}
+
+// Inclusive sum over the lanes below and at this one.
+__device__ __forceinline__ int wave_scan(int x) {
+  const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4 *>(&lds.o[w][r][d0]);
-    float rm = lds.row[r][0], rl = lds.row[r][1];
-    if (bad) rm = rl = __builtin_nanf("");
-    if (!direct) {
-      *reinterpret_cast<f32x4 *>(a.part_o + ((int64_t)part * all_rows + out_row) * D + d0) = v;
-      if (d0 == 0) a.part_ml[(int64_t)part * all_rows + out_row] = float2{rm, rl};
-    } else {
-      // No key at all: zeros.
-      const bool none = !bad && len - n_new + tk + 1 <= 0;
-      const float inv = none ? 0.f : 1.f / rl;
-      u32x2 w;
-      w.x = none ? 0u : pack16<DT>(v[0] * inv, v[1] * inv);
-      w.y = none ? 0u : pack16<DT>(v[2] * inv, v[3] * inv);
-      *reinterpret_cast<u32x2 *>(a.out + out_row * D + d0) = w;
-      if (d0 == 0 && a.lse != nullptr)
-        a.lse[(int64_t)(out_row % a.n_q_heads) * a.plan.tokens + out_row / a.n_q_heads] =
-            none ? kNegInf : (rm + __builtin_log2f(rl)) * 0.6931471805599453f;
+  for (int s = 1; s < 64; s <<= 1) {
+    const int y = __shfl_up(x, s);
+    x += lane >= s ? y : 0;
+  }
+  return x;
+}
+
+// Steps of a group's run: ceil(all sequences' steps / groups), at least 1.
+// Every lane of the wave calls it.
+template <int D, int FMT>
+__device__ __forceinline__ int run_steps(const DecodeAttnArgs &a) {
+  const int lane = threadIdx.x & 63;
+  int mine = 0;
+  for (int b = lane; b < a.batch.batch; b += 64) mine += steps_of<D, FMT>(own_len(a, b));
+  const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);
+  return max(1, (total + a.plan.groups - 1) / a.plan.groups);
+}
+
+// Item `item`: KV head item % n_kv_heads of row tile and chunk (SHARED) or
+// group of waves.
+template <int D, int FMT, int DT, bool SHARED>
+__device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int64_t id, int row_tiles, char *smem) {
+  using G = Geo<D, FMT>;
+  // In a scalar register, and with it every condition that only the wave decides.
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  NarrowLds &lds = reinterpret_cast<NarrowLds *>(smem)[wave];
+  const int64_t item = id * kWaves + wave;
+  int unit = (int)(item / a.pool.n_kv_heads);
+  const int kvh = (int)(item - (int64_t)unit * a.pool.n_kv_heads);
+  const int tile = unit % row_tiles;
+  unit /= row_tiles;
+  if constexpr (SHARED) {
+    if (unit >= a.plan.shared_chunks) return;                // the last workgroup's waves without an item
+    const int k0 = unit * a.plan.shared_chunk, len = a.batch.shared_len;
+    narrow_keys<D, FMT, DT, true>(a, 0, len, k0, min(len, k0 + a.plan.shared_chunk), kvh, tile,
+                                  (int64_t)unit * a.plan.tokens * a.n_q_heads, lds);
+  } else if (a.plan.direct) {
+    if (unit >= a.batch.batch) return;
+    const int len = own_len(a, unit);
+    narrow_keys<D, FMT, DT, false>(a, unit, len, 0, len, kvh, tile, 0, lds);
+  } else {
+    if (unit >= a.plan.groups) return;
+    const int per = run_steps<D, FMT>(a);
+    const int first = unit * per;                            // the run's steps [first, first + per); all fit 2^30
+    const int64_t rows = (int64_t)a.batch.n_new * a.n_q_heads;
+    const int64_t own0 = (int64_t)a.plan.shared_chunks * a.plan.tokens * a.n_q_heads;
+    int before = 0;                                          // steps of the sequences before the lanes'
+    for (int b0 = 0; b0 < a.batch.batch && before < first + per; b0 += 64) {
+      const int len = b0 + lane < a.batch.batch ? own_len(a, b0 + lane) : 0;
+      const int steps = steps_of<D, FMT>(len);
+      const int upto = wave_scan(steps);
+      const int begin = before + upto - steps;
+      uint64_t todo = __builtin_amdgcn_ballot_w64(steps > 0 && begin < first + per && begin + steps > first);
+      while (todo != 0) {
+        const int l = __builtin_ctzll(todo);
+        todo &= todo - 1;
+        const int n = __builtin_amdgcn_readlane(len, l);
+        const int s0 = before + __builtin_amdgcn_readlane(upto - steps, l);
+        const int k0 = max(0, first - s0) * G::kStep;
+        const int k1 = (int)min((int64_t)n, (int64_t)(first + per - s0) * G::kStep);
+        narrow_keys<D, FMT, DT, false>(a, b0 + l, n, k0, k1, kvh, tile, own0 + (int64_t)(unit + b0 + l) * rows, lds);
+      }
+      before += __builtin_amdgcn_readlane(upto, 63);
     }
   }
 }
@@ -790,21 +827,41 @@ __global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(DecodeAttnArgs
 // Merge.  D / 4 lanes hold a row's output, 4 dims each; `split` such lane
 // groups of a workgroup share one row's partials.
 // ---------------------------------------------------------------------------
-template <int D, int DT>
-__global__ __launch_bounds__(kThreads) void decode_merge_kernel(DecodeAttnArgs a, int split) {
-  constexpr int kLanes = D / 4, kSlots = kThreads / kLanes;
+template <int D, int FMT, int DT>
+__global__ __launch_bounds__(kMergeThreads) void decode_merge_kernel(DecodeAttnArgs a, int split) {
+  constexpr int kLanes = D / 4, kSlots = kMergeThreads / kLanes;
   __shared__ __attribute__((aligned(16))) float s_o[kSlots][D];
   __shared__ float s_ml[kSlots][2];
   const int slot = threadIdx.x / kLanes, d0 = 4 * (threadIdx.x % kLanes);
   const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
-  const int64_t row = (int64_t)blockIdx.x * (kSlots / split) + slot / split;
+  const int64_t row = ((int64_t)blockIdx.x * blockDim.x / kLanes + slot) / split;
   const bool in = row < all_rows;
   const int token = in ? (int)(row / a.n_q_heads) : 0, head = in ? (int)(row - (int64_t)token * a.n_q_heads) : 0;
-  const int seq = token / a.batch.n_new;
+  const int seq = token / a.batch.n_new, tok_in = token - seq * a.batch.n_new;
   const int len = own_len(a, seq);
-  const int limit = len - a.batch.n_new + (token - seq * a.batch.n_new) + 1;
-  const int own = len > 0 ? (len + a.plan.own_chunk - 1) / a.plan.own_chunk : 0;
-  const int parts = in && len >= 0 ? a.plan.shared_chunks + own : 0;
+  const int limit = len - a.batch.n_new + tok_in + 1;
+  // The sequence's steps and, of the groups' runs, the first and the number
+  // that touch them.
+  const int lane = threadIdx.x & 63;
+  int sum = 0;                               // steps of all sequences in this lane's stride
+  int begin = 0;                             // steps before each lane's row's sequence
+  const int steps = steps_of<D, FMT>(len);
+  for (int b0 = 0; b0 < a.batch.batch; b0 += 64) {
+    const int s = b0 + lane < a.batch.batch ? steps_of<D, FMT>(own_len(a, b0 + lane)) : 0;
+    const int upto = wave_scan(s);
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    const int here = __shfl(upto - s, seq & 63);
+    if (seq >= b0 + 64) begin += all;
+    if (seq >= b0 && seq < b0 + 64) begin += here;
+    sum += all;
+  }
+  const int per = max(1, (sum + a.plan.groups - 1) / a.plan.groups);
+  const int r0 = begin / per, own = steps > 0 ? (begin + steps - 1) / per - r0 + 1 : 0;
+  const int shared = a.plan.shared_chunks;
+  const int parts = in && len >= 0 ? shared + own : 0;
+  const int64_t seq_rows = (int64_t)a.batch.n_new * a.n_q_heads;
+  const int64_t own0 = shared * all_rows + (int64_t)(r0 + seq) * seq_rows + (int64_t)tok_in * a.n_q_heads + head;
+  auto row_of = [&](int p) { return p < shared ? p * all_rows + row : own0 + (p - shared) * seq_rows; };
 
   float m = kNegInf, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -815,7 +872,7 @@ __global__ __launch_bounds__(kThreads) void decode_merge_kernel(DecodeAttnArgs a
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       const bool have = p + i * split < parts;
-      const int64_t at = (int64_t)(have ? p + i * split : p) * all_rows + row;
+      const int64_t at = row_of(have ? p + i * split : p);
       ml[i] = a.part_ml[at];
       v[i] = *reinterpret_cast<const f32x4 *>(a.part_o + at * D + d0);
       if (!have) ml[i] = float2{kNegInf, 0.f}, v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -865,8 +922,8 @@ __global__ __launch_bounds__(kThreads) void decode_merge_kernel(DecodeAttnArgs a
 template <int D, int FMT, int DT, bool WIDE>
 hipError_t launch_chunks(const DecodeAttnArgs &a, hipStream_t stream) {
   const DecodePlan &pl = a.plan;
-  constexpr size_t lds = WIDE ? wide_lds_bytes<D>() : sizeof(NarrowLds<D>);
-  static_assert(lds >= sizeof(NarrowLds<D>), "both bodies' LDS");
+  constexpr size_t lds = WIDE ? wide_lds_bytes<D>() : kWaves * sizeof(NarrowLds);
+  static_assert(lds >= kWaves * sizeof(NarrowLds), "both bodies' LDS");
   const void *kernel = reinterpret_cast<const void *>(&decode_attn_kernel<D, FMT, DT, WIDE>);
   if (lds > 64 * 1024) {
     static std::atomic<uint64_t> ready{0};   // devices on which the kernel may use that much LDS
@@ -884,8 +941,10 @@ hipError_t launch_chunks(const DecodeAttnArgs &a, hipStream_t stream) {
   const int shared_rows = WIDE ? kWideRows : 16;
   const int shared_tiles = (pl.tokens * pl.group + shared_rows - 1) / shared_rows;
   const int own_tiles = (pl.rows + 15) / 16;
-  const int shared_groups = heads * shared_tiles * pl.shared_chunks;
-  const int64_t groups = shared_groups + (int64_t)heads * own_tiles * pl.own_chunks * a.batch.batch;
+  auto narrow_groups = [&](int64_t units) { return (units * heads + kWaves - 1) / kWaves; };
+  const int shared_groups = WIDE ? heads * shared_tiles * pl.shared_chunks
+                                 : (int)narrow_groups((int64_t)shared_tiles * pl.shared_chunks);
+  const int64_t groups = shared_groups + narrow_groups((int64_t)own_tiles * (pl.direct ? a.batch.batch : pl.groups));
   hipLaunchKernelGGL((decode_attn_kernel<D, FMT, DT, WIDE>), dim3((unsigned)groups), dim3(kThreads), lds, stream, a,
                      shared_groups, shared_tiles, own_tiles);
   return hipGetLastError();
@@ -897,12 +956,15 @@ hipError_t launch_all(const DecodeAttnArgs &a, hipStream_t stream) {
   const hipError_t e = pl.shared_wide && pl.shared_chunks > 0 ? launch_chunks<D, FMT, DT, true>(a, stream)
                                                               : launch_chunks<D, FMT, DT, false>(a, stream);
   if (e != hipSuccess || pl.direct) return e;
-  constexpr int slots = kThreads / (D / 4);
+  // A row's partials: all shared chunks, and the own keys' share of the groups
+  // if the sequences were equally long (the rows of longer ones loop).
+  const int parts = pl.shared_chunks + (pl.groups + a.batch.batch - 1) / a.batch.batch;
+  constexpr int lanes = D / 4;
   int split = 1;
-  while (split < slots && 2 * split <= pl.max_parts) split *= 2;
-  const int64_t all_rows = (int64_t)pl.tokens * a.n_q_heads;
-  const int per = slots / split;
-  hipLaunchKernelGGL((decode_merge_kernel<D, DT>), dim3((unsigned)((all_rows + per - 1) / per)), dim3(kThreads), 0,
+  while (split < kMergeThreads / lanes && 4 * split <= parts) split *= 2;
+  const int threads = std::max(kThreads, split * lanes);
+  const int64_t per = threads / lanes / split, all_rows = (int64_t)pl.tokens * a.n_q_heads;
+  hipLaunchKernelGGL((decode_merge_kernel<D, FMT, DT>), dim3((unsigned)((all_rows + per - 1) / per)), dim3(threads), 0,
                      stream, a, split);
   return hipGetLastError();
 }

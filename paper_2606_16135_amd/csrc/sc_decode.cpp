@@ -89,7 +89,7 @@ sc_status check_batch(const sc_pool *pool, const sc_decode_batch *b, bool pointe
   if (b->batch <= 0 || b->n_new < 1 || b->n_new > 16 || b->max_blocks < 0 || b->max_len < 0 || b->shared_len < 0)
     return fail(SC_ERR_INVALID, "decode batch: batch %d, n_new %d (1..16), max_blocks %d, max_len %d, shared_len %d",
                 b->batch, b->n_new, b->max_blocks, b->max_len, b->shared_len);
-  if ((int64_t)b->batch * b->n_new > INT32_MAX) return fail(SC_ERR_RANGE, "too many tokens in a decode step");
+  if (b->batch > 65536) return fail(SC_ERR_RANGE, "a decode step of %d sequences (at most 65536)", b->batch);
   if ((int64_t)b->max_len + b->shared_len > INT32_MAX - 257)
     return fail(SC_ERR_RANGE, "%d shared and %d own tokens exceed 32-bit positions", b->shared_len, b->max_len);
   if (!pointers) return SC_OK;
@@ -110,17 +110,11 @@ DecodeView view_of(const sc_decode_batch *b) {
                     b->n_new,     b->max_blocks, b->max_len,    b->shared_len};
 }
 
-// Keys of a chunk so that `lists` key lists of `len` keys, read by `per`
-// workgroups per chunk, give about `target` workgroups: a multiple of
-// `unit`, at least `least`.
-int chunk_keys(int64_t len, int64_t per, int64_t target, int unit, int least) {
-  const int64_t chunks = std::max<int64_t>(1, target / std::max<int64_t>(1, per));
-  const int64_t keys = std::max<int64_t>(least, (len + chunks - 1) / chunks);
-  return (int)std::min<int64_t>((keys + unit - 1) / unit * unit, (int64_t)1 << 30);
-}
-
 constexpr int kDecodeCus = 256;              // MI355X
 constexpr int kNarrowRows = 16;
+// Waves that read own keys: two per SIMD, what a CU holds of them.
+constexpr int kDecodeWaves = 8 * kDecodeCus;
+constexpr int kMaxDecodeGroups = 1 << 23;    // workgroups of a launch
 
 sc_status plan_decode(const sc_pool *pool, const sc_decode_batch *b, int hq, DecodePlan *out) {
   const int hkv = pool->desc.n_kv_heads;
@@ -129,33 +123,45 @@ sc_status plan_decode(const sc_pool *pool, const sc_decode_batch *b, int hq, Dec
   if (hq / hkv > 16) return fail(SC_ERR_UNSUPPORTED, "GQA group %d > 16 not supported", hq / hkv);
   if ((int64_t)b->batch * b->n_new * hq > INT32_MAX)
     return fail(SC_ERR_RANGE, "%d x %d tokens of %d heads exceed 32-bit rows", b->batch, b->n_new, hq);
+  const int step = decode_step_keys(pool->desc.head_dim, pool->kv_format);
   DecodePlan p{};
   p.group = hq / hkv;
   p.rows = b->n_new * p.group;
   p.tokens = b->batch * b->n_new;
   const int64_t all_rows = (int64_t)p.tokens * p.group;
   p.shared_wide = all_rows > kNarrowRows;
+  int64_t shared_items = 0;
   if (b->shared_len > 0) {
+    // Wide: about two workgroups per CU.  Narrow: a wave per step, up to two
+    // per SIMD.
     const int64_t tiles = p.shared_wide ? (all_rows + 127) / 128 : 1;
-    p.shared_chunk = chunk_keys(b->shared_len, tiles * hkv, 2 * kDecodeCus, 128, 256);
+    const int64_t chunks = std::max<int64_t>(1, (p.shared_wide ? 2 * kDecodeCus : kDecodeWaves) / (tiles * hkv));
+    const int64_t unit = p.shared_wide ? 128 : step;
+    const int64_t keys = std::max<int64_t>(p.shared_wide ? 256 : step, (b->shared_len + chunks - 1) / chunks);
+    p.shared_chunk = (int32_t)std::min<int64_t>((keys + unit - 1) / unit * unit, (int64_t)1 << 30);
     p.shared_chunks = (b->shared_len + p.shared_chunk - 1) / p.shared_chunk;
+    shared_items = tiles * hkv * p.shared_chunks;
   }
-  const int64_t row_tiles = (p.rows + kNarrowRows - 1) / kNarrowRows;
-  p.own_chunk = chunk_keys(b->max_len, row_tiles * hkv * b->batch, 4 * kDecodeCus, 64, 256);
-  p.own_chunks = std::max(1, (int)(((int64_t)b->max_len + p.own_chunk - 1) / p.own_chunk));
-  p.direct = b->shared_len == 0 && p.own_chunks == 1;
-  p.max_parts = p.shared_chunks + p.own_chunks;
-  const int64_t own_groups = row_tiles * hkv * b->batch * p.own_chunks;
-  const int64_t shared_groups = (all_rows + kNarrowRows - 1) / kNarrowRows * hkv * std::max(1, p.shared_chunks);
-  if (own_groups > (1 << 23) || shared_groups > (1 << 23))
+  // Own keys: as many groups as the device holds waves, but no more than
+  // there can be steps.
+  const int64_t heads = (int64_t)hkv * ((p.rows + kNarrowRows - 1) / kNarrowRows);
+  const int64_t steps = (int64_t)b->batch * std::max<int64_t>(1, ((int64_t)b->max_len + step - 1) / step);
+  if (steps > (1 << 30))   // the device adds the sequences' steps in 32 bits
+    return fail(SC_ERR_RANGE, "%d sequences of up to %d tokens are too many keys for a decode step", b->batch, b->max_len);
+  p.groups = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kDecodeWaves / heads, steps));
+  p.direct = b->shared_len == 0 && b->max_len <= step;
+  if (heads * std::max<int64_t>(p.groups, p.direct ? b->batch : 0) > kMaxDecodeGroups || shared_items > kMaxDecodeGroups ||
+      (all_rows + 15) / 16 * hkv > kMaxDecodeGroups)
     return fail(SC_ERR_RANGE, "a decode step of %d sequences x %d KV heads needs too many workgroups", b->batch, hkv);
   *out = p;
   return SC_OK;
 }
 
 // Partial outputs, then their (maximum, sum) pairs.
-size_t workspace_bytes_of(const DecodePlan &p, int hq, int head_dim, size_t *ml_off) {
-  const size_t rows = p.direct ? 0 : (size_t)p.max_parts * p.tokens * hq;
+size_t workspace_bytes_of(const DecodePlan &p, const sc_decode_batch *b, int hq, int head_dim, size_t *ml_off) {
+  const size_t seq_rows = (size_t)b->n_new * hq;
+  const size_t rows =
+      p.direct ? 0 : (size_t)p.shared_chunks * b->batch * seq_rows + ((size_t)p.groups + b->batch) * seq_rows;
   *ml_off = rows * head_dim * sizeof(float);
   return *ml_off + rows * sizeof(float2);
 }
@@ -335,7 +341,7 @@ sc_status sc_decode_workspace(const sc_pool *pool, const sc_decode_batch *batch,
   st = plan_decode(pool, batch, n_q_heads, &plan);
   if (st != SC_OK) return st;
   size_t ml;
-  *bytes = workspace_bytes_of(plan, n_q_heads, pool->desc.head_dim, &ml);
+  *bytes = workspace_bytes_of(plan, batch, n_q_heads, pool->desc.head_dim, &ml);
   return SC_OK;
 }
 
@@ -354,7 +360,7 @@ sc_status sc_decode_attn(sc_pool *pool, int32_t layer, const sc_decode_batch *ba
   if (!aligned(q, 16) || !aligned(out, 16)) return fail(SC_ERR_INVALID, "q and out must be 16-byte aligned");
   if (!aligned(lse, 4)) return fail(SC_ERR_INVALID, "lse must be 4-byte aligned");
   size_t ml_off = 0;
-  const size_t need = workspace_bytes_of(a.plan, n_q_heads, d.head_dim, &ml_off);
+  const size_t need = workspace_bytes_of(a.plan, batch, n_q_heads, d.head_dim, &ml_off);
   if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
     return fail(SC_ERR_INVALID, "the call needs a 256-byte aligned workspace of %zu bytes (got %zu)", need,
                 workspace_bytes);

@@ -182,18 +182,28 @@ struct DecodeStoreArgs {
 };
 hipError_t launch_decode_store(const DecodeStoreArgs &a, hipStream_t stream);
 
-// Work of one decode-attention call (see plan_decode).  The key chunks of
-// the shared prefix come first, then those of the sequences' own tokens;
-// partial p of a row is its p-th chunk's.
+// Keys of a wave's step over a list (decode_attn.hip): 16 KiB of K and V.
+inline constexpr int decode_step_keys(int head_dim, int kv_format) {
+  return head_dim == 128 && kv_format == SC_KV_16BIT ? 32 : 64;
+}
+
+// Work of one decode-attention call (see plan_decode).  Partials of a row:
+// one per chunk of the shared prefix, and one per group of waves that reads
+// a part of the row's own keys.
+//
+// Own keys: the steps of all sequences, one after another, are dealt to
+// `groups` groups of waves (one wave per KV head and row tile) in equal runs
+// of `per` = ceil(steps / groups) steps, which only the device knows (it has
+// the lengths).  Group r's part of sequence b is partial r + b of n_new *
+// n_q_heads rows: along the runs either the group or the sequence goes up.
 struct DecodePlan {
   int32_t group;              // query heads per KV head
   int32_t rows;               // rows of one sequence and KV head: n_new * group
   int32_t tokens;             // batch * n_new
-  int32_t own_chunk, own_chunks;        // keys of a chunk, chunks of max_len (at least one)
+  int32_t groups;
   int32_t shared_chunk, shared_chunks;
   int32_t shared_wide;        // the shared keys by the kernel for more than 16 rows
-  int32_t direct;             // one chunk and no shared prefix: no partials
-  int32_t max_parts;          // partials of a row: shared_chunks + own_chunks
+  int32_t direct;             // no shared prefix and one step a sequence: one group each, no partials
 };
 struct DecodeAttnArgs {
   PoolView pool;
@@ -202,8 +212,11 @@ struct DecodeAttnArgs {
   const uint16_t *q;
   uint16_t *out;
   float *lse;
-  float *part_o;          // [max_parts][tokens * n_q_heads][head_dim], not divided by the sums
-  float2 *part_ml;        // [max_parts][tokens * n_q_heads]: running maximum (log2 domain) and sum
+  // Shared chunks' partials [shared_chunks][tokens * n_q_heads], then the own
+  // keys' [groups + batch][n_new * n_q_heads]: outputs of head_dim floats, not
+  // divided by the sums, and (maximum in the log2 domain, sum).
+  float *part_o;
+  float2 *part_ml;
   int32_t n_q_heads;
   float scale_log2;
 };

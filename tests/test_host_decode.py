@@ -92,7 +92,7 @@ def test_calls_without_objects(sc):
 BATCHES = [
     (dict(batch=0), "INVALID"), (dict(batch=-1), "INVALID"), (dict(n_new=0), "INVALID"), (dict(n_new=17), "INVALID"),
     (dict(max_blocks=-1), "INVALID"), (dict(max_len=-1), "INVALID"), (dict(shared_len=-1), "INVALID"),
-    (dict(batch=1 << 30, n_new=4), "RANGE"), (dict(max_len=2**31 - 257), "RANGE"),
+    (dict(batch=65537), "RANGE"), (dict(max_len=2**31 - 257), "RANGE"),
     (dict(max_len=2**30, shared_len=2**30), "RANGE"),
 ]
 POINTERS = [dict(kv_len=0), dict(block_ids=0), dict(shared_len=5, shared_ids=0), dict(kv_len=FAKE + 2),
@@ -142,19 +142,23 @@ def test_decode_argument_refusals(sc, pool):
     refused(sc, "INVALID", store, p, 0, b, FAKE, 0)
     refused(sc, "INVALID", store, p, 0, b, FAKE + 8, FAKE)
     refused(sc, "INVALID", store, p, 0, b, FAKE, FAKE, 0, FAKE, 32, FAKE, text="rotary")   # q, nothing to turn it by
-    refused(sc, "RANGE", attn, p, 0, batch_of(sc, batch=1 << 28), FAKE, 32, FAKE, FAKE, 1 << 60)
-    refused(sc, "RANGE", attn, p, 0, batch_of(sc, batch=1 << 22), FAKE, 32, FAKE, FAKE, 1 << 60)   # workgroups
+    refused(sc, "RANGE", attn, p, 0, batch_of(sc, batch=1 << 16, max_len=1 << 30), FAKE, 32, FAKE, FAKE, 1 << 60)
+    wide = pool(heads=1 << 12)
+    refused(sc, "RANGE", attn, wide, 0, batch_of(sc, batch=1 << 16, n_new=16), FAKE, 1 << 12, FAKE, FAKE, 1 << 62)
 
 
 def test_workspace_grows_with_the_batch_and_is_nothing_for_one_chunk(sc, pool):
     p = pool()
-    assert sc.sc_decode_workspace(p, batch_of(sc, max_len=64), 32) == 0
+    assert sc.sc_decode_workspace(p, batch_of(sc, max_len=32), 32) == 0
     assert sc.sc_decode_workspace(p, batch_of(sc, max_len=0, max_blocks=0), 32) == 0
-    a = sc.sc_decode_workspace(p, batch_of(sc, batch=1, max_len=50000), 32)
-    row = 32 * (128 * 4 + 8)
-    assert a % row == 0 and a // row >= 8
-    shared = sc.sc_decode_workspace(p, batch_of(sc, max_len=64, shared_len=1), 32)
-    assert shared == 2 * 2 * row                                               # a shared and an own partial a row
+    row = 32 * (128 * 4 + 8)                      # one sequence's partials
+    # two sequences of up to two steps: four groups of waves, a partial per group and sequence boundary
+    assert sc.sc_decode_workspace(p, batch_of(sc, max_len=64), 32) == (4 + 2) * row
+    # long ones: what the device holds, 2048 waves over 8 KV heads
+    assert sc.sc_decode_workspace(p, batch_of(sc, batch=1, max_len=50000), 32) == (256 + 1) * row
+    # with a shared prefix: its chunk's partials of both sequences too
+    assert sc.sc_decode_workspace(p, batch_of(sc, max_len=32, shared_len=1), 32) == (2 + 2 + 2) * row
+    assert sc.sc_decode_workspace(pool(sc.SC_KV_E4M3), batch_of(sc, max_len=64), 32) == 0     # steps of 64 keys
 
 
 def test_register_check_covers_the_copy_kernels_of_byte_sized_blocks():
