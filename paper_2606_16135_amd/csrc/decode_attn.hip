@@ -28,12 +28,9 @@
 // A wave takes 16 KiB of K and V at a time.
 //
 // Wide (wide_body): more rows than that share the keys (a shared prefix:
-// every row of the batch).  A workgroup of four waves of 32 rows takes
-// 128-key tiles through LDS: the tile is loaded to registers while the one
-// before is computed, then converted to 16 bits (8-bit codes are exact in
-// bf16 and fp16) and written to LDS in operand order, so that the key loop
-// reads whole 16-byte operands and an 8-bit tile is converted once for all
-// rows.
+// every row of the batch).  A workgroup takes 256 rows through 128-key tiles
+// in LDS, where a tile is laid out in operand order, 8-bit codes converted to
+// 16 bits (exact in bf16 and fp16) once for all rows.
 //
 // 8-bit K and V: a key's scales are applied to its score and to its
 // probability, in fp32.  The probabilities are rounded to the element type
@@ -59,10 +56,10 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;             // of a workgroup without a wide part
+constexpr int kWideWaves = 8;
 constexpr int kTile = 128;            // keys of a workgroup's tile (wide)
-constexpr int kWideRows = 128;
+constexpr int kWideRows = 32 * kWideWaves;
 constexpr int kMergeThreads = 1024;   // at most
 constexpr float kNegInf = -__builtin_inff();
 
@@ -527,12 +524,12 @@ __device__ __forceinline__ int run_steps(const DecodeAttnArgs &a) {
 // Item `item`: KV head item % n_kv_heads of row tile and chunk (SHARED) or
 // group of waves.
 template <int D, int FMT, int DT, bool SHARED>
-__device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int64_t id, int row_tiles, char *smem) {
+__device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int64_t first_item, int row_tiles, char *smem) {
   using G = Geo<D, FMT>;
   // In a scalar register, and with it every condition that only the wave decides.
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   NarrowLds &lds = reinterpret_cast<NarrowLds *>(smem)[wave];
-  const int64_t item = id * kWaves + wave;
+  const int64_t item = first_item + wave;
   int unit = (int)(item / a.pool.n_kv_heads);
   const int kvh = (int)(item - (int64_t)unit * a.pool.n_kv_heads);
   const int tile = unit % row_tiles;
@@ -574,19 +571,41 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int64_t id,
 }
 
 // ---------------------------------------------------------------------------
-// Wide: one chunk of the shared keys, one KV head, 128 rows of the batch.
+// Wide: one chunk of the shared keys, one KV head, 256 rows of the batch.
+//
+// Eight waves of 32 rows share 128-key tiles in two LDS buffers with one
+// barrier a tile: while tile t is computed, tile t + 1 goes from the loaders'
+// registers into the other buffer (waves 0-3 load and lay out V, waves 4-7 K)
+// and tile t + 2 is loaded.  LDS holds whole MFMA operands, 16 bytes a lane.
+//
+// The vector unit is the bound (per score half a maximum, an FMA, an
+// exponential, an add and half a pack, for 8-bit blocks a multiplication by
+// each of K's and V's scales, against 32 MFMA cycles for 16 of them), so the
+// reference m of a row's softmax, which may be any number, is not its running
+// maximum: it moves only when a score exceeds it by kRefSlack (in the log2
+// domain), and only then do lanes exchange anything and the accumulators
+// change.  The slack keeps the probabilities inside fp16.
 // ---------------------------------------------------------------------------
+constexpr float kRefSlack = 12.f;
+
+template <int D>
+struct WideLds {
+  u32x4 k[2][kTile * D / 8];                 // [buffer][tile of 16 keys][step][lane]
+  u32x4 v[2][kTile * D / 8];                 // [buffer][32 keys][operand][lane]
+  float scale[2][2][kTile];                  // [buffer][K times the softmax scale, V]
+  uint64_t addr[2][kTile];
+  int bad[2];
+};
+
 template <int D, int FMT, int DT>
 __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int row_tiles, char *smem) {
   using G = Geo<D, FMT>;
   constexpr int kPv = pv_type<FMT, DT>();
-  constexpr int kKPer = kTile * G::kRow / 16 / kThreads;      // 16-byte K pieces of a thread
+  constexpr int kKThreads = 256;
+  constexpr int kKPer = kTile * G::kRow / 16 / kKThreads;     // 16-byte K pieces of a loader
   constexpr int kPieces = G::kRow / 16;                       // ... of a key
-  u32x4 *const s_k = reinterpret_cast<u32x4 *>(smem);         // [8][D / 32][64] operands
-  u32x4 *const s_v = s_k + kTile * D / 8;                     // [4][D / 16][64]
-  uint64_t(*const s_addr)[kTile] = reinterpret_cast<uint64_t(*)[kTile]>(s_v + kTile * D / 8);   // [2]
-  float(*const s_scale)[kTile] = reinterpret_cast<float(*)[kTile]>(s_addr + 2);                 // [2]: K, V
-  int *const s_bad = reinterpret_cast<int *>(s_scale + 2);   // [2], tiles of one parity: set while the other is read
+  static_assert(kKPer <= 8 && kWideWaves == 8, "eight registers of 16 bytes hold a loader's part of a tile");
+  WideLds<D> &lds = *reinterpret_cast<WideLds<D> *>(smem);
 
   const PoolView &p = a.pool;
   const int kvh = id % p.n_kv_heads;
@@ -620,38 +639,49 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
 
   const int64_t head_off = (int64_t)kvh * G::kRow;
   const int64_t row_bytes = (int64_t)p.n_kv_heads * G::kRow;
+  const bool loads_v = wave < 4;             // and addresses and scales; the others load K
   const int my_key = tid & (kTile - 1);      // threads 0..127: K's scale, 128..255: V's
-  if (tid < 2) s_bad[tid] = 0;
+  if (tid < 2) lds.bad[tid] = 0;
   __syncthreads();
   int32_t next_id = 0;                       // block of this thread's key of the tile to address next
-  auto fetch_id = [&](int t) { next_id = a.batch.shared_ids[block_of(p, min(k0 + t * kTile + my_key, k1 - 1))]; };
-  const char *my_scale = nullptr;            // of the tile whose address was taken last
+  auto fetch_id = [&](int t) {
+    if (loads_v) next_id = a.batch.shared_ids[block_of(p, min(k0 + t * kTile + my_key, k1 - 1))];
+  };
+  uint64_t my_scale = 0, next_scale = 0;     // this thread's scale of the tile to load next, and after it
   auto take_addr = [&](int t) {              // address of this thread's key of tile t
+    if (!loads_v) return;
     const int key = min(k0 + t * kTile + my_key, k1 - 1);
     const char *base = block_layer(p, next_id);
     if (base == nullptr) {
-      s_bad[t & 1] = 1;
+      lds.bad[t & 1] = 1;
       return;
     }
     const int in_block = key - block_of(p, key) * p.block_size;
-    if (tid < kTile) s_addr[t & 1][my_key] = reinterpret_cast<uint64_t>(base + in_block * row_bytes + head_off);
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    if (tid < kTile) lds.addr[t & 1][my_key] = at + in_block * row_bytes + head_off;
     if constexpr (G::k8)
-      my_scale = base + (tid < kTile ? 0 : p.half_bytes) + p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
+      next_scale = at + (tid < kTile ? 0 : p.half_bytes) + p.scale_off + ((int64_t)in_block * p.n_kv_heads + kvh) * 2;
   };
-  u32x4 kr[kKPer];
-  Words<G::kVWords> vr[8];
+  u32x4 raw[8];                              // the tile in flight: K pieces or V keys
   uint32_t scale_bits = 0;
   auto load_tile = [&](int t) {
+    if (loads_v) {
 #pragma unroll
-    for (int i = 0; i < kKPer; ++i) {
-      const int idx = tid + kThreads * i;
-      kr[i] = load_global<u32x4>(s_addr[t & 1][idx / kPieces] + 16 * (idx % kPieces));
+      for (int j = 0; j < 8; ++j) {
+        const Words<G::kVWords> w =
+            load_words<G::kVWords>(lds.addr[t & 1][32 * wave + 16 * (j >> 2) + 4 * g + (j & 3)] + p.half_bytes +
+                                   n * (G::kVd * G::kElem));
+#pragma unroll
+        for (int q = 0; q < G::kVWords; ++q) raw[j][q] = w.w[q];
+      }
+      if constexpr (G::k8) scale_bits = load_global<uint16_t>(my_scale);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kKPer; ++i) {
+        const int idx = tid - kKThreads + kKThreads * i;
+        raw[i] = load_global<u32x4>(lds.addr[t & 1][idx / kPieces] + 16 * (idx % kPieces));
+      }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      vr[j] = load_words<G::kVWords>(s_addr[t & 1][32 * wave + 16 * (j >> 2) + 4 * g + (j & 3)] + p.half_bytes +
-                                     n * (G::kVd * G::kElem));
-    if constexpr (G::k8) scale_bits = load_global<uint16_t>(reinterpret_cast<uint64_t>(my_scale));
   };
   // Position of lane (m, g)'s K operand of step c: rotated among the 16 keys
   // so that the pieces of one key, which consecutive threads write, fall on
@@ -660,128 +690,176 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
     return (t16 * G::kSteps + c) * 64 + g_ * 16 + (m_ ^ ((4 * c + g_) & 15));
   };
   auto write_tile = [&](int t) {
+    u32x4 *const sk = lds.k[t & 1], *const sv = lds.v[t & 1];
+    if (loads_v) {
+      if (k0 + (t + 1) * kTile > k1) {       // no value for the keys behind the last: not a copy of its
 #pragma unroll
-    for (int i = 0; i < kKPer; ++i) {
-      const int idx = tid + kThreads * i;
-      const int key = idx / kPieces, x = idx % kPieces;
-      if constexpr (!G::k8) {
-        s_k[k_slot(key >> 4, x >> 2, x & 3, key & 15)] = kr[i];
-      } else {
+        for (int j = 0; j < 8; ++j)
+          if (k0 + t * kTile + 32 * wave + 16 * (j >> 2) + 4 * g + (j & 3) >= k1) raw[j] = u32x4{0, 0, 0, 0};
+      }
+      Words<G::kVWords> vr[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float f0[4], f1[4];
-          codes_to_f32<FMT>(kr[i][2 * h], f0);
-          codes_to_f32<FMT>(kr[i][2 * h + 1], f1);
-          s_k[k_slot(key >> 4, 2 * (x >> 2) + h, x & 3, key & 15)] =
-              u32x4{pack16<DT>(f0[0], f0[1]), pack16<DT>(f0[2], f0[3]), pack16<DT>(f1[0], f1[1]),
-                    pack16<DT>(f1[2], f1[3])};
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int q = 0; q < G::kVWords; ++q) vr[j].w[q] = raw[j][q];
+      u32x4 vo[G::kVd];
+      v_operands<D, FMT>(vr, vo);
+#pragma unroll
+      for (int d = 0; d < G::kVd; ++d) sv[(wave * G::kVd + d) * 64 + lane] = vo[d];
+      if constexpr (G::k8)
+        lds.scale[t & 1][tid / kTile][my_key] =
+            __builtin_bit_cast(float, scale_bits << 16) * (tid < kTile ? a.scale_log2 : 1.f);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kKPer; ++i) {
+        const int idx = tid - kKThreads + kKThreads * i;
+        const int key = idx / kPieces, x = idx % kPieces;
+        if constexpr (!G::k8) {
+          sk[k_slot(key >> 4, x >> 2, x & 3, key & 15)] = raw[i];
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float f0[4], f1[4];
+            codes_to_f32<FMT>(raw[i][2 * h], f0);
+            codes_to_f32<FMT>(raw[i][2 * h + 1], f1);
+            sk[k_slot(key >> 4, 2 * (x >> 2) + h, x & 3, key & 15)] =
+                u32x4{pack16<DT>(f0[0], f0[1]), pack16<DT>(f0[2], f0[3]), pack16<DT>(f1[0], f1[1]),
+                      pack16<DT>(f1[2], f1[3])};
+          }
         }
       }
     }
-    if (k0 + (t + 1) * kTile > k1) {         // no value for the keys behind the last: not a copy of its
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (k0 + t * kTile + 32 * wave + 16 * (j >> 2) + 4 * g + (j & 3) >= k1)
-#pragma unroll
-          for (int q = 0; q < G::kVWords; ++q) vr[j].w[q] = 0;
-    }
-    u32x4 vo[G::kVd];
-    v_operands<D, FMT>(vr, vo);
-#pragma unroll
-    for (int d = 0; d < G::kVd; ++d) s_v[(wave * G::kVd + d) * 64 + lane] = vo[d];
-    if constexpr (G::k8) s_scale[tid / kTile][my_key] = __builtin_bit_cast(float, scale_bits << 16);
   };
 
   RowState st[2] = {{kNegInf, 0.f}, {kNegInf, 0.f}};
+  float neg_ref[2] = {0.f, 0.f};             // -m, or 0 while there is none
+  float limit[2] = {kNegInf, kNegInf};       // a score above it moves m
   f32x4 o[2][G::kVd];
 #pragma unroll
   for (int r = 0; r < 2; ++r)
 #pragma unroll
     for (int d = 0; d < G::kVd; ++d) o[r][d] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+  auto compute = [&](int t, int u) {         // keys 32 u .. 32 u + 31 of tile t
+    const u32x4 *const sk = lds.k[t & 1], *const sv = lds.v[t & 1];
+    f32x4 s[2][2];
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      s[0][tt] = s[1][tt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < G::kSteps; ++c) {
+        const u32x4 kf = sk[k_slot(2 * u + tt, c, g, n)];
+        s[0][tt] = mfma16<DT>(kf, qf[0][c], s[0][tt]);
+        s[1][tt] = mfma16<DT>(kf, qf[1][c], s[1][tt]);
+      }
+    }
+    const int base = k0 + t * kTile + 32 * u;
+    const bool edge = base + 32 > k1;
+    f32x4 ks[2], vs[2];                      // scales of the lane's keys
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      ks[tt] = f32x4{a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
+      if constexpr (G::k8) {
+        ks[tt] = *reinterpret_cast<const f32x4 *>(&lds.scale[t & 1][0][32 * u + 16 * tt + 4 * g]);
+        vs[tt] = *reinterpret_cast<const f32x4 *>(&lds.scale[t & 1][1][32 * u + 16 * tt + 4 * g]);
+      }
+    }
+    if (edge) {                              // keys behind the last: no score, whatever their scales are
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (base + 16 * tt + 4 * g + i >= k1) {
+            s[0][tt][i] = s[1][tt][i] = kNegInf;
+            ks[tt][i] = 1.f;
+            if constexpr (G::k8) vs[tt][i] = 0.f;
+          }
+    }
+    u32x4 pf[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = G::k8 ? s[r][i >> 2][i & 3] * ks[i >> 2][i & 3] : s[r][i >> 2][i & 3];
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if constexpr (!G::k8) top *= a.scale_log2;
+      if (wave_any(top > limit[r])) {        // a new reference for the rows that need one
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float m = fmaxf(st[r].m, top);
+        const float alpha = __builtin_amdgcn_exp2f(st[r].m - m);   // m is finite or +infinity here, or both are -infinity
+        const float f = m == kNegInf ? 1.f : alpha;
+        st[r].m = m;
+        st[r].l *= f;
+        limit[r] = m + kRefSlack;
+        neg_ref[r] = m == kNegInf ? 0.f : -m;
+#pragma unroll
+        for (int d = 0; d < G::kVd; ++d) o[r][d] *= f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i >> 2][i & 3], ks[i >> 2][i & 3], neg_ref[r]));
+        st[r].l += x[i];
+      }
+      if constexpr (G::k8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] *= vs[i >> 2][i & 3];
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) pf[r][q] = pack16<kPv>(x[2 * q], x[2 * q + 1]);
+    }
+#pragma unroll
+    for (int d = 0; d < G::kVd; ++d) {
+      const u32x4 vf = sv[(u * G::kVd + d) * 64 + lane];
+      o[0][d] = mfma16<kPv>(vf, pf[0], o[0][d]);
+      o[1][d] = mfma16<kPv>(vf, pf[1], o[1][d]);
+    }
+  };
+
+  // Tile t is addressed in iteration t - 3, loaded in t - 2, written in t - 1;
+  // its address slot and its bad flag are those of its parity, and a barrier
+  // lies between every use by one tile and the next one's.
+  int end = tiles;                           // tiles before the first bad id
+  auto check = [&](int t) {
+    if (t < end && lds.bad[t & 1] != 0) end = t;
+  };
   fetch_id(0);
   take_addr(0);
   if (tiles > 1) fetch_id(1);
   __syncthreads();
-  bool bad = s_bad[0] != 0;
-  if (!bad) {
+  check(0);
+  if (end > 0) {
+    my_scale = next_scale;
     load_tile(0);
     if (tiles > 1) take_addr(1);
-  }
-  for (int t = 0; t < tiles && !bad; ++t) {
-    if (t + 2 < tiles) fetch_id(t + 2);      // older than the loads below, so that waiting for it leaves them in flight
-    __syncthreads();                         // the operands of tile t - 1 have been read
-    write_tile(t);
+    if (tiles > 2) fetch_id(2);
+    write_tile(0);
     __syncthreads();
-    const bool next_bad = s_bad[(t + 1) & 1] != 0;
-    if (t + 1 < tiles && !next_bad) load_tile(t + 1);
-    if (busy) {
-#pragma unroll 1
-      for (int h = 0; h < 2; ++h) {          // 64 keys at a time
-        float x[2][16];
-#pragma unroll
-        for (int tt = 0; tt < 4; ++tt) {
-          f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-          for (int c = 0; c < G::kSteps; ++c) {
-            const u32x4 kf = s_k[k_slot(4 * h + tt, c, g, n)];
-            s[0] = mfma16<DT>(kf, qf[0][c], s[0]);
-            s[1] = mfma16<DT>(kf, qf[1][c], s[1]);
-          }
-          f32x4 sc = {a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
-          if constexpr (G::k8) sc *= *reinterpret_cast<const f32x4 *>(&s_scale[0][64 * h + 16 * tt + 4 * g]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[0][4 * tt + i] = s[0][i] * sc[i];
-            x[1][4 * tt + i] = s[1][i] * sc[i];
-          }
-        }
-        const int base = k0 + t * kTile + 64 * h;
-        const bool edge = base + 64 > k1;
-        if (edge) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (base + 16 * (i >> 2) + 4 * g + (i & 3) >= k1) x[0][i] = x[1][i] = kNegInf;
-        }
-        u32x4 pf[2][2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const float alpha = softmax_step(x[r], st[r]);
-          if (wave_any(alpha != 1.f)) {
-#pragma unroll
-            for (int d = 0; d < G::kVd; ++d) o[r][d] *= alpha;
-          }
-          if constexpr (G::k8) {
-#pragma unroll
-            for (int tt = 0; tt < 4; ++tt) {
-              const f32x4 sc = *reinterpret_cast<const f32x4 *>(&s_scale[1][64 * h + 16 * tt + 4 * g]);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) x[r][4 * tt + i] *= sc[i];
-            }
-            if (edge) {                      // 0 x a NaN scale
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                if (base + 16 * (i >> 2) + 4 * g + (i & 3) >= k1) x[r][i] = 0.f;
-            }
-          }
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) pf[r][u][q] = pack16<kPv>(x[r][8 * u + 2 * q], x[r][8 * u + 2 * q + 1]);
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int d = 0; d < G::kVd; ++d) {
-            const u32x4 vf = s_v[((2 * h + u) * G::kVd + d) * 64 + lane];
-            o[0][d] = mfma16<kPv>(vf, pf[0][u], o[0][d]);
-            o[1][d] = mfma16<kPv>(vf, pf[1][u], o[1][d]);
-          }
-      }
-    }
-    bad = next_bad;
-    if (!bad && t + 2 < tiles) take_addr(t + 2);
+    check(1);
+    my_scale = next_scale;
+    if (end > 1) load_tile(1);
+    if (end > 1 && tiles > 2) take_addr(2);
+    __syncthreads();
+    check(2);
   }
+  for (int t = 0; t < end; ++t) {
+    if (t + 3 < end) fetch_id(t + 3);
+    if (busy) {
+      compute(t, 0);
+      compute(t, 1);
+    }
+    if (t + 1 < end) write_tile(t + 1);
+    my_scale = next_scale;
+    if (t + 2 < end) load_tile(t + 2);
+    if (busy) {
+      compute(t, 2);
+      compute(t, 3);
+    }
+    if (t + 3 < end) take_addr(t + 3);
+    __syncthreads();
+    check(t + 3);
+  }
+  const bool bad = end < tiles;
 
   const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
 #pragma unroll
@@ -802,25 +880,23 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   }
 }
 
-template <int D>
-constexpr size_t wide_lds_bytes() {
-  return 2 * (size_t)kTile * D * 2 + 2 * kTile * sizeof(uint64_t) + 2 * kTile * sizeof(float) + 16;
-}
-
 // One launch for both key lists, the shared one's workgroups first: they are
 // the longer ones, and the own keys' loads fill the memory's time beside the
 // wide kernel's matrix work.  WIDE: the shared keys have more than 16 rows.
 template <int D, int FMT, int DT, bool WIDE>
-__global__ __launch_bounds__(kThreads, 2) void decode_attn_kernel(DecodeAttnArgs a, int shared_groups, int shared_tiles,
-                                                                  int own_tiles) {
+__global__ __launch_bounds__(64 * (WIDE ? kWideWaves : kWaves), 2) void decode_attn_kernel(DecodeAttnArgs a,
+                                                                                          int shared_groups,
+                                                                                          int shared_tiles,
+                                                                                          int own_tiles) {
+  constexpr int kGroupWaves = WIDE ? kWideWaves : kWaves;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int id = blockIdx.x;
   if (id >= shared_groups)
-    narrow_body<D, FMT, DT, false>(a, id - shared_groups, own_tiles, smem);
+    narrow_body<D, FMT, DT, false>(a, (int64_t)(id - shared_groups) * kGroupWaves, own_tiles, smem);
   else if constexpr (WIDE)
     wide_body<D, FMT, DT>(a, id, shared_tiles, smem);
   else
-    narrow_body<D, FMT, DT, true>(a, id, shared_tiles, smem);
+    narrow_body<D, FMT, DT, true>(a, (int64_t)id * kGroupWaves, shared_tiles, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -922,8 +998,9 @@ __global__ __launch_bounds__(kMergeThreads) void decode_merge_kernel(DecodeAttnA
 template <int D, int FMT, int DT, bool WIDE>
 hipError_t launch_chunks(const DecodeAttnArgs &a, hipStream_t stream) {
   const DecodePlan &pl = a.plan;
-  constexpr size_t lds = WIDE ? wide_lds_bytes<D>() : kWaves * sizeof(NarrowLds);
-  static_assert(lds >= kWaves * sizeof(NarrowLds), "both bodies' LDS");
+  constexpr int waves = WIDE ? kWideWaves : kWaves;
+  constexpr size_t lds = WIDE ? sizeof(WideLds<D>) : waves * sizeof(NarrowLds);
+  static_assert(lds >= waves * sizeof(NarrowLds), "both bodies' LDS");
   const void *kernel = reinterpret_cast<const void *>(&decode_attn_kernel<D, FMT, DT, WIDE>);
   if (lds > 64 * 1024) {
     static std::atomic<uint64_t> ready{0};   // devices on which the kernel may use that much LDS
@@ -941,11 +1018,11 @@ hipError_t launch_chunks(const DecodeAttnArgs &a, hipStream_t stream) {
   const int shared_rows = WIDE ? kWideRows : 16;
   const int shared_tiles = (pl.tokens * pl.group + shared_rows - 1) / shared_rows;
   const int own_tiles = (pl.rows + 15) / 16;
-  auto narrow_groups = [&](int64_t units) { return (units * heads + kWaves - 1) / kWaves; };
+  auto narrow_groups = [&](int64_t units) { return (units * heads + waves - 1) / waves; };
   const int shared_groups = WIDE ? heads * shared_tiles * pl.shared_chunks
                                  : (int)narrow_groups((int64_t)shared_tiles * pl.shared_chunks);
   const int64_t groups = shared_groups + narrow_groups((int64_t)own_tiles * (pl.direct ? a.batch.batch : pl.groups));
-  hipLaunchKernelGGL((decode_attn_kernel<D, FMT, DT, WIDE>), dim3((unsigned)groups), dim3(kThreads), lds, stream, a,
+  hipLaunchKernelGGL((decode_attn_kernel<D, FMT, DT, WIDE>), dim3((unsigned)groups), dim3(64 * waves), lds, stream, a,
                      shared_groups, shared_tiles, own_tiles);
   return hipGetLastError();
 }
@@ -962,7 +1039,7 @@ hipError_t launch_all(const DecodeAttnArgs &a, hipStream_t stream) {
   constexpr int lanes = D / 4;
   int split = 1;
   while (split < kMergeThreads / lanes && 4 * split <= parts) split *= 2;
-  const int threads = std::max(kThreads, split * lanes);
+  const int threads = std::max(256, split * lanes);
   const int64_t per = threads / lanes / split, all_rows = (int64_t)pl.tokens * a.n_q_heads;
   hipLaunchKernelGGL((decode_merge_kernel<D, FMT, DT>), dim3((unsigned)((all_rows + per - 1) / per)), dim3(threads), 0,
                      stream, a, split);

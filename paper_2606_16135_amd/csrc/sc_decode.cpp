@@ -132,10 +132,10 @@ sc_status plan_decode(const sc_pool *pool, const sc_decode_batch *b, int hq, Dec
   p.shared_wide = all_rows > kNarrowRows;
   int64_t shared_items = 0;
   if (b->shared_len > 0) {
-    // Wide: about two workgroups per CU.  Narrow: a wave per step, up to two
+    // Wide: a workgroup per CU.  Narrow: a wave per step, up to two
     // per SIMD.
-    const int64_t tiles = p.shared_wide ? (all_rows + 127) / 128 : 1;
-    const int64_t chunks = std::max<int64_t>(1, (p.shared_wide ? 2 * kDecodeCus : kDecodeWaves) / (tiles * hkv));
+    const int64_t tiles = p.shared_wide ? (all_rows + 255) / 256 : 1;
+    const int64_t chunks = std::max<int64_t>(1, (p.shared_wide ? kDecodeCus : kDecodeWaves) / (tiles * hkv));
     const int64_t unit = p.shared_wide ? 128 : step;
     const int64_t keys = std::max<int64_t>(p.shared_wide ? 256 : step, (b->shared_len + chunks - 1) / chunks);
     p.shared_chunk = (int32_t)std::min<int64_t>((keys + unit - 1) / unit * unit, (int64_t)1 << 30);
