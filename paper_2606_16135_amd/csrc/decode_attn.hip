@@ -620,8 +620,14 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int rows = a.plan.tokens * group;
-  const int row0 = tile * kWideRows + wave * 32;
-  const bool busy = row0 < rows;             // this wave has rows
+  // Fewer rows than eight waves have: row_waves (a power of two) of them
+  // cover the rows, and the others share their keys, every key_waves-th
+  // 32-key block each.  64 rows over 65536 bf16 keys 49 us, 79 with a wave's
+  // keys unshared: two busy waves a CU took longer for a tile than its load.
+  const int rows_here = min(kWideRows, rows - tile * kWideRows);
+  const int row_waves = rows_here > 128 ? 8 : rows_here > 64 ? 4 : rows_here > 32 ? 2 : 1;
+  const int key_waves = kWideWaves / row_waves, key_wave = wave / row_waves;
+  const int row0 = tile * kWideRows + (wave & (row_waves - 1)) * 32;
   int64_t out_row[2];
   bool has_row[2];
   u32x4 qf[2][G::kSteps];
@@ -819,6 +825,7 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   // Tile t is addressed in iteration t - 3, loaded in t - 2, written in t - 1;
   // its address slot and its bad flag are those of its parity, and a barrier
   // lies between every use by one tile and the next one's.
+  auto mine = [&](int u) { return (u & (key_waves - 1)) == key_wave; };
   int end = tiles;                           // tiles before the first bad id
   auto check = [&](int t) {
     if (t < end && lds.bad[t & 1] != 0) end = t;
@@ -844,39 +851,75 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   }
   for (int t = 0; t < end; ++t) {
     if (t + 3 < end) fetch_id(t + 3);
-    if (busy) {
-      compute(t, 0);
-      compute(t, 1);
-    }
+    if (mine(0)) compute(t, 0);
+    if (mine(1)) compute(t, 1);
     if (t + 1 < end) write_tile(t + 1);
     my_scale = next_scale;
     if (t + 2 < end) load_tile(t + 2);
-    if (busy) {
-      compute(t, 2);
-      compute(t, 3);
-    }
+    if (mine(2)) compute(t, 2);
+    if (mine(3)) compute(t, 3);
     if (t + 3 < end) take_addr(t + 3);
     __syncthreads();
     check(t + 3);
   }
   const bool bad = end < tiles;
+  const float nan = __builtin_nanf("");
 
   const int64_t all_rows = (int64_t)a.plan.tokens * a.n_q_heads;
+  // The keys' waves meet in LDS, which no tile needs any more.
+  constexpr int kJoinRow = D + 4;            // floats of a row, padded against bank conflicts
+  float *const join_o = reinterpret_cast<float *>(smem);
+  float2 *const join_ml = reinterpret_cast<float2 *>(&lds.scale[0][0][0]);
+  static_assert(sizeof(lds.scale) >= kWideWaves * 32 * sizeof(float2), "one pair a wave and row");
+  static_assert(sizeof(lds.k) + sizeof(lds.v) >= kWideWaves * 16 * kJoinRow * sizeof(float), "one half of the rows");
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
     float l = st[r].l;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (!has_row[r]) continue;
-    const int64_t at = (int64_t)chunk * all_rows + out_row[r];
+    if (key_waves == 1) {
+      if (!has_row[r]) continue;
+      const int64_t at = (int64_t)chunk * all_rows + out_row[r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[G::kVd];
+#pragma unroll
+        for (int d = 0; d < G::kVd; ++d) v[d] = o[r][d][i];
+        store_f32(a.part_o + at * D + G::kVd * (4 * g + i), v);
+      }
+      if (g == 0) a.part_ml[at] = bad ? float2{nan, nan} : float2{st[r].m, l};
+      continue;
+    }
+    if (r == 1) __syncthreads();             // the first half of the rows has been read
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v[G::kVd];
 #pragma unroll
       for (int d = 0; d < G::kVd; ++d) v[d] = o[r][d][i];
-      store_f32(a.part_o + at * D + G::kVd * (4 * g + i), v);
+      store_f32(join_o + (wave * 16 + n) * kJoinRow + G::kVd * (4 * g + i), v);
     }
-    if (g == 0) a.part_ml[at] = bad ? float2{__builtin_nanf(""), __builtin_nanf("")} : float2{st[r].m, l};
+    if (g == 0) join_ml[wave * 16 + n] = float2{st[r].m, l};
+    __syncthreads();
+    // Thread: 4 dims of one of the 16 row_waves rows.
+    for (int idx = tid; idx < row_waves * 16 * (D / 4); idx += 64 * kWideWaves) {
+      const int jr = idx / (D / 4), d0 = 4 * (idx % (D / 4));          // jr = 16 * row wave + row
+      const int row = tile * kWideRows + (jr >> 4) * 32 + 16 * r + (jr & 15);
+      if (row >= rows) continue;
+      float m = kNegInf, sum = 0.f;
+      for (int w = 0; w < key_waves; ++w) m = fmaxf(m, join_ml[w * row_waves * 16 + jr].x);
+      const float ref = m == kNegInf ? 0.f : m;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < key_waves; ++w) {
+        const float2 ml = join_ml[w * row_waves * 16 + jr];
+        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+        sum += f * ml.y;
+        v += f * *reinterpret_cast<const f32x4 *>(join_o + (w * row_waves * 16 + jr) * kJoinRow + d0);
+      }
+      const int token = row / group;
+      const int64_t at = (int64_t)chunk * all_rows + (int64_t)token * a.n_q_heads + kvh * group + (row - token * group);
+      *reinterpret_cast<f32x4 *>(a.part_o + at * D + d0) = v;
+      if (d0 == 0) a.part_ml[at] = bad ? float2{nan, nan} : float2{m, sum};
+    }
   }
 }
 

@@ -115,6 +115,14 @@ constexpr int kNarrowRows = 16;
 // Waves that read own keys: two per SIMD, what a CU holds of them.
 constexpr int kDecodeWaves = 8 * kDecodeCus;
 constexpr int kMaxDecodeGroups = 1 << 23;    // workgroups of a launch
+// The wide part's tile of rows and keys, and the times a CU takes for one,
+// measured: 256 rows 5.3 us (64 x 4 rows of 5 heads over 32768 bf16 keys),
+// few rows 2.5 us (the tile's loads); and what a CU reads of own keys.
+constexpr int kWideRows = 256, kWideKeys = 128;
+constexpr double kWideTileUs = 2.5, kWideRowUs = 5.7 / 256, kCuBytesPerUs = 22e3;
+// From a workgroup's start to its first tile; writing and reading partials.
+constexpr double kStartUs = 8, kPartBytesPerUs = 4e6;
+constexpr int64_t kMinOwnCus = 32;
 
 sc_status plan_decode(const sc_pool *pool, const sc_decode_batch *b, int hq, DecodePlan *out) {
   const int hkv = pool->desc.n_kv_heads;
@@ -131,24 +139,49 @@ sc_status plan_decode(const sc_pool *pool, const sc_decode_batch *b, int hq, Dec
   const int64_t all_rows = (int64_t)p.tokens * p.group;
   p.shared_wide = all_rows > kNarrowRows;
   int64_t shared_items = 0;
-  if (b->shared_len > 0) {
-    // Wide: a workgroup per CU.  Narrow: a wave per step, up to two
-    // per SIMD.
-    const int64_t tiles = p.shared_wide ? (all_rows + 255) / 256 : 1;
-    const int64_t chunks = std::max<int64_t>(1, (p.shared_wide ? kDecodeCus : kDecodeWaves) / (tiles * hkv));
-    const int64_t unit = p.shared_wide ? 128 : step;
-    const int64_t keys = std::max<int64_t>(p.shared_wide ? 256 : step, (b->shared_len + chunks - 1) / chunks);
-    p.shared_chunk = (int32_t)std::min<int64_t>((keys + unit - 1) / unit * unit, (int64_t)1 << 30);
+  const int64_t heads = (int64_t)hkv * ((p.rows + kNarrowRows - 1) / kNarrowRows);
+  int64_t own_waves = kDecodeWaves;
+  if (b->shared_len > 0 && p.shared_wide) {
+    // A workgroup per CU, a wide one leaves a CU no room for another.  Of the
+    // chunk counts that fit, the one whose estimate ends first: the own keys
+    // beside the wide workgroups on the CUs those leave, or after them.  (The
+    // own keys count in full: their lengths are not known here.)
+    const int64_t tiles = (all_rows + kWideRows - 1) / kWideRows;
+    const int64_t key_tiles = ((int64_t)b->shared_len + kWideKeys - 1) / kWideKeys;
+    const double tile_us = std::max(kWideTileUs, kWideRowUs * (double)std::min<int64_t>(all_rows, kWideRows));
+    const double own_us = (double)b->batch * b->max_len * (double)heads * (double)(pool->row_bytes / hkv) * 2 / kCuBytesPerUs;
+    const int64_t most = std::max<int64_t>(1, std::min(key_tiles, kDecodeCus / (tiles * hkv)));
+    int64_t chunks = 1;
+    double best = 0;
+    for (int64_t c = 1; c <= most; ++c) {
+      const int64_t groups = tiles * hkv * c, free = kDecodeCus - groups;
+      const double wide_us = tile_us * (double)((key_tiles + c - 1) / c) * (double)((groups + kDecodeCus - 1) / kDecodeCus);
+      const bool beside = free >= kMinOwnCus;
+      const double parts_us = (double)(c * p.tokens * hq) * pool->desc.head_dim * 8 / kPartBytesPerUs;
+      const double us = parts_us + kStartUs + (beside ? std::max(wide_us, own_us / (double)free)
+                                                      : wide_us + kStartUs + own_us / kDecodeCus);
+      if (c > 1 && us >= best) continue;
+      best = us;
+      chunks = c;
+      own_waves = beside && own_us / (double)free <= 1.1 * wide_us + 5 ? 8 * free : kDecodeWaves;
+    }
+    p.shared_chunk = (int32_t)((key_tiles + chunks - 1) / chunks * kWideKeys);
     p.shared_chunks = (b->shared_len + p.shared_chunk - 1) / p.shared_chunk;
     shared_items = tiles * hkv * p.shared_chunks;
+  } else if (b->shared_len > 0) {
+    // A wave per step, up to two per SIMD.
+    const int64_t steps = ((int64_t)b->shared_len + step - 1) / step;
+    const int64_t chunks = std::min<int64_t>(steps, std::max(1, kDecodeWaves / hkv));
+    p.shared_chunk = (int32_t)((steps + chunks - 1) / chunks * step);
+    p.shared_chunks = (b->shared_len + p.shared_chunk - 1) / p.shared_chunk;
+    shared_items = (int64_t)hkv * p.shared_chunks;
   }
   // Own keys: as many groups as the device holds waves, but no more than
   // there can be steps.
-  const int64_t heads = (int64_t)hkv * ((p.rows + kNarrowRows - 1) / kNarrowRows);
   const int64_t steps = (int64_t)b->batch * std::max<int64_t>(1, ((int64_t)b->max_len + step - 1) / step);
   if (steps > (1 << 30))   // the device adds the sequences' steps in 32 bits
     return fail(SC_ERR_RANGE, "%d sequences of up to %d tokens are too many keys for a decode step", b->batch, b->max_len);
-  p.groups = (int32_t)std::max<int64_t>(1, std::min<int64_t>(kDecodeWaves / heads, steps));
+  p.groups = (int32_t)std::max<int64_t>(1, std::min<int64_t>(own_waves / heads, steps));
   p.direct = b->shared_len == 0 && b->max_len <= step;
   if (heads * std::max<int64_t>(p.groups, p.direct ? b->batch : 0) > kMaxDecodeGroups || shared_items > kMaxDecodeGroups ||
       (all_rows + 15) / 16 * hkv > kMaxDecodeGroups)
