@@ -33,9 +33,14 @@
 // 16 bits (exact in bf16 and fp16) once for all rows.
 //
 // 8-bit K and V: a key's scales are applied to its score and to its
-// probability, in fp32.  The probabilities are rounded to the element type
-// for the PV product, with 8-bit blocks always to bf16: scaled by a row's
-// scale they may be far below what fp16 holds, and the codes need 8 bits.
+// probability, in fp32; the codes, exact in either type, go into the products.
+// The probabilities are rounded to the element type for the PV product.  With
+// 8-bit blocks and fp16 that product 2^(s_j - m) v_scale_j could leave fp16's
+// range either way, so there m is the maximum of s_j + log2 v_scale_j (the
+// logarithm cut to kMaxLogScale): the rounded factors are then at most 1, and
+// what is lost below fp16's normal numbers is 2^-24 of the largest.  The sums
+// l, which hold no v_scale, stay in fp32's range: 2^-40 to 2^40 per key.  bf16
+// has fp32's range and needs none of this.
 //
 // Keys past a row's end: scores are replaced by -infinity (never computed
 // with), probabilities by 0 after scaling, and where such keys are in a tile
@@ -146,7 +151,7 @@ __device__ __forceinline__ u32x4 k_operand(const u32x4 (&raw)[Geo<D, FMT>::kLoad
 }
 
 // V operands of 8 keys: operand d holds dim d of every key.
-template <int D, int FMT>
+template <int D, int FMT, int DT>
 __device__ __forceinline__ void v_operands(const Words<Geo<D, FMT>::kVWords> (&raw)[8], u32x4 (&op)[D / 16]) {
   using G = Geo<D, FMT>;
   if constexpr (!G::k8) {
@@ -167,15 +172,19 @@ __device__ __forceinline__ void v_operands(const Words<Geo<D, FMT>::kVWords> (&r
         codes_to_f32<FMT>(raw[2 * p].w[w], a);
         codes_to_f32<FMT>(raw[2 * p + 1].w[w], b);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) op[4 * w + i][p] = pack16<SC_DTYPE_BF16>(a[i], b[i]);
+        for (int i = 0; i < 4; ++i) op[4 * w + i][p] = pack16<DT>(a[i], b[i]);
       }
   }
 }
 
-// Element type of the PV product.
-template <int FMT, int DT>
-constexpr int pv_type() {
-  return FMT == SC_KV_16BIT ? DT : SC_DTYPE_BF16;
+// Whether the reference of a softmax takes in V's scales, and a scale's part.
+template <int D, int FMT, int DT>
+constexpr bool weigh_scales() {
+  return Geo<D, FMT>::k8 && DT == SC_DTYPE_F16;
+}
+constexpr float kMaxLogScale = 40.f;
+__device__ __forceinline__ float log_scale(float s) {          // (finite for a NaN too)
+  return fminf(fmaxf(__builtin_amdgcn_logf(s), -kMaxLogScale), kMaxLogScale);
 }
 
 // Keys of sequence b in its own blocks; -1 for an empty slot, kBad for a
@@ -205,13 +214,14 @@ struct RowState {
   float m, l;
 };
 
-// p = 2^(x - m) for the lane's N scores of one row; the row's four lanes
-// agree on m.  Returns the factor for what was accumulated before.
-template <int N>
-__device__ __forceinline__ float softmax_step(float (&x)[N], RowState &st) {
-  float top = x[0];
+// p = 2^(x - m) for the lane's N scores of one row, where m is at least the
+// largest `key(i)`; the row's four lanes agree on it.  Returns the factor for
+// what was accumulated before.
+template <int N, class Key>
+__device__ __forceinline__ float softmax_step(float (&x)[N], RowState &st, Key key) {
+  float top = key(0);
 #pragma unroll
-  for (int i = 1; i < N; ++i) top = fmaxf(top, x[i]);
+  for (int i = 1; i < N; ++i) top = fmaxf(top, key(i));
   top = fmaxf(top, __shfl_xor(top, 16));
   top = fmaxf(top, __shfl_xor(top, 32));
   const float m = fmaxf(st.m, top);
@@ -253,7 +263,7 @@ __device__ __forceinline__ void store_f32(float *p, const float (&v)[N]) {
 // ---------------------------------------------------------------------------
 struct NarrowLds {                           // of one wave
   uint64_t addr[64];
-  float scale[2][64];
+  float scale[3][64];                        // K, V, log_scale(V)
 };
 
 // Keys [k0, k1) of sequence `seq`, as partial `part` of its rows.
@@ -261,7 +271,6 @@ template <int D, int FMT, int DT, bool SHARED>
 __device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, int len, int k0, int k1, int kvh, int tile,
                                             int64_t part, NarrowLds &lds) {
   using G = Geo<D, FMT>;
-  constexpr int kPv = pv_type<FMT, DT>();
   constexpr int kStep = G::kStep, kTiles = kStep / 16, kHalves = kStep / 32;
   const PoolView &p = a.pool;
   const int lane = threadIdx.x & 63;
@@ -334,6 +343,7 @@ __device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, in
     if constexpr (G::k8) {
       lds.scale[0][lane] = __builtin_bit_cast(float, ks << 16);
       lds.scale[1][lane] = __builtin_bit_cast(float, vs << 16);
+      if constexpr (weigh_scales<D, FMT, DT>()) lds.scale[2][lane] = log_scale(__builtin_bit_cast(float, vs << 16));
     }
     wave_lds_order();
   };
@@ -392,7 +402,14 @@ __device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, in
         for (int i = 0; i < 4; ++i)
           if (base + 16 * t + 4 * g + i >= min(limit, k1)) x[4 * t + i] = kNegInf;
     }
-    const float alpha = softmax_step(x, st);
+    f32x4 lv[kTiles];
+    if constexpr (weigh_scales<D, FMT, DT>())
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) lv[t] = *reinterpret_cast<const f32x4 *>(&lds.scale[2][16 * t + 4 * g]);
+    const float alpha = softmax_step(x, st, [&](int i) {
+      if constexpr (weigh_scales<D, FMT, DT>()) return x[i] + lv[i >> 2][i & 3];
+      else return x[i];
+    });
     if (wave_any(alpha != 1.f)) {
 #pragma unroll
       for (int d = 0; d < G::kVd; ++d) o[d] *= alpha;
@@ -417,12 +434,12 @@ __device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, in
           if (base + 32 * u + 16 * (j >> 2) + 4 * g + (j & 3) >= min(limit, k1)) w[j] = 0.f;
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) pf[q] = pack16<kPv>(w[2 * q], w[2 * q + 1]);
+      for (int q = 0; q < 4; ++q) pf[q] = pack16<DT>(w[2 * q], w[2 * q + 1]);
       u32x4 vo[G::kVd];
       if (!edge) {
-        v_operands<D, FMT>(vr[u], vo);
+        v_operands<D, FMT, DT>(vr[u], vo);
 #pragma unroll
-        for (int d = 0; d < G::kVd; ++d) o[d] = mfma16<kPv>(vo[d], pf, o[d]);
+        for (int d = 0; d < G::kVd; ++d) o[d] = mfma16<DT>(vo[d], pf, o[d]);
       } else {
         // One pass per distinct end: V without the keys that this token does
         // not see, added to its rows only.
@@ -436,11 +453,11 @@ __device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, in
 #pragma unroll
             for (int q = 0; q < G::kVWords; ++q) cut[j].w[q] = hidden ? 0u : vr[u][j].w[q];
           }
-          v_operands<D, FMT>(cut, vo);
+          v_operands<D, FMT, DT>(cut, vo);
           const bool mine = SHARED || tok_in == tk;
 #pragma unroll
           for (int d = 0; d < G::kVd; ++d) {
-            const f32x4 add = mfma16<kPv>(vo[d], pf, f32x4{0.f, 0.f, 0.f, 0.f});
+            const f32x4 add = mfma16<DT>(vo[d], pf, f32x4{0.f, 0.f, 0.f, 0.f});
             if (mine) o[d] += add;
           }
         }
@@ -582,7 +599,8 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int64_t fir
 // exponential, an add and half a pack, for 8-bit blocks a multiplication by
 // each of K's and V's scales, against 32 MFMA cycles for 16 of them), so the
 // reference m of a row's softmax, which may be any number, is not its running
-// maximum: it moves only when a score exceeds it by kRefSlack (in the log2
+// maximum: it moves only when a score (with its part of V's scale, see the top)
+// exceeds it by kRefSlack (in the log2
 // domain), and only then do lanes exchange anything and the accumulators
 // change.  The slack keeps the probabilities inside fp16.
 // ---------------------------------------------------------------------------
@@ -592,7 +610,7 @@ template <int D>
 struct WideLds {
   u32x4 k[2][kTile * D / 8];                 // [buffer][tile of 16 keys][step][lane]
   u32x4 v[2][kTile * D / 8];                 // [buffer][32 keys][operand][lane]
-  float scale[2][2][kTile];                  // [buffer][K times the softmax scale, V]
+  float scale[2][3][kTile];                  // [buffer][K times the softmax scale, V, log_scale(V)]
   uint64_t addr[2][kTile];
   int bad[2];
 };
@@ -600,7 +618,6 @@ struct WideLds {
 template <int D, int FMT, int DT>
 __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int row_tiles, char *smem) {
   using G = Geo<D, FMT>;
-  constexpr int kPv = pv_type<FMT, DT>();
   constexpr int kKThreads = 256;
   constexpr int kKPer = kTile * G::kRow / 16 / kKThreads;     // 16-byte K pieces of a loader
   constexpr int kPieces = G::kRow / 16;                       // ... of a key
@@ -622,7 +639,7 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   const int rows = a.plan.tokens * group;
   // Fewer rows than eight waves have: row_waves (a power of two) of them
   // cover the rows, and the others share their keys, every key_waves-th
-  // 32-key block each.  64 rows over 65536 bf16 keys 49 us, 79 with a wave's
+  // 32-key block each.  64 rows over 65536 bf16 keys 68 us, 79 with a wave's
   // keys unshared: two busy waves a CU took longer for a tile than its load.
   const int rows_here = min(kWideRows, rows - tile * kWideRows);
   const int row_waves = rows_here > 128 ? 8 : rows_here > 64 ? 4 : rows_here > 32 ? 2 : 1;
@@ -709,12 +726,14 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
 #pragma unroll
         for (int q = 0; q < G::kVWords; ++q) vr[j].w[q] = raw[j][q];
       u32x4 vo[G::kVd];
-      v_operands<D, FMT>(vr, vo);
+      v_operands<D, FMT, DT>(vr, vo);
 #pragma unroll
       for (int d = 0; d < G::kVd; ++d) sv[(wave * G::kVd + d) * 64 + lane] = vo[d];
-      if constexpr (G::k8)
-        lds.scale[t & 1][tid / kTile][my_key] =
-            __builtin_bit_cast(float, scale_bits << 16) * (tid < kTile ? a.scale_log2 : 1.f);
+      if constexpr (G::k8) {
+        const float s = __builtin_bit_cast(float, scale_bits << 16);
+        lds.scale[t & 1][tid / kTile][my_key] = s * (tid < kTile ? a.scale_log2 : 1.f);
+        if (weigh_scales<D, FMT, DT>() && tid >= kTile) lds.scale[t & 1][2][my_key] = log_scale(s);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < kKPer; ++i) {
@@ -761,13 +780,15 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
     }
     const int base = k0 + t * kTile + 32 * u;
     const bool edge = base + 32 > k1;
-    f32x4 ks[2], vs[2];                      // scales of the lane's keys
+    f32x4 ks[2], vs[2], lv[2];               // scales of the lane's keys
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       ks[tt] = f32x4{a.scale_log2, a.scale_log2, a.scale_log2, a.scale_log2};
       if constexpr (G::k8) {
         ks[tt] = *reinterpret_cast<const f32x4 *>(&lds.scale[t & 1][0][32 * u + 16 * tt + 4 * g]);
         vs[tt] = *reinterpret_cast<const f32x4 *>(&lds.scale[t & 1][1][32 * u + 16 * tt + 4 * g]);
+        if constexpr (weigh_scales<D, FMT, DT>())
+          lv[tt] = *reinterpret_cast<const f32x4 *>(&lds.scale[t & 1][2][32 * u + 16 * tt + 4 * g]);
       }
     }
     if (edge) {                              // keys behind the last: no score, whatever their scales are
@@ -786,7 +807,11 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
     for (int r = 0; r < 2; ++r) {
       float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = G::k8 ? s[r][i >> 2][i & 3] * ks[i >> 2][i & 3] : s[r][i >> 2][i & 3];
+      for (int i = 0; i < 8; ++i) {
+        const float y = s[r][i >> 2][i & 3];
+        if constexpr (weigh_scales<D, FMT, DT>()) x[i] = __builtin_fmaf(y, ks[i >> 2][i & 3], lv[i >> 2][i & 3]);
+        else x[i] = G::k8 ? y * ks[i >> 2][i & 3] : y;
+      }
       float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
       if constexpr (!G::k8) top *= a.scale_log2;
       if (wave_any(top > limit[r])) {        // a new reference for the rows that need one
@@ -812,13 +837,13 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
         for (int i = 0; i < 8; ++i) x[i] *= vs[i >> 2][i & 3];
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) pf[r][q] = pack16<kPv>(x[2 * q], x[2 * q + 1]);
+      for (int q = 0; q < 4; ++q) pf[r][q] = pack16<DT>(x[2 * q], x[2 * q + 1]);
     }
 #pragma unroll
     for (int d = 0; d < G::kVd; ++d) {
       const u32x4 vf = sv[(u * G::kVd + d) * 64 + lane];
-      o[0][d] = mfma16<kPv>(vf, pf[0], o[0][d]);
-      o[1][d] = mfma16<kPv>(vf, pf[1], o[1][d]);
+      o[0][d] = mfma16<DT>(vf, pf[0], o[0][d]);
+      o[1][d] = mfma16<DT>(vf, pf[1], o[1][d]);
     }
   };
 

@@ -141,14 +141,15 @@ def scale_bits(s):
 
 
 def attention_bound(ref, absv, mag, dtype, fmt, t, vmax):
-    """|out - ref| from: each probability rounded once to the PV product's
-    type (half a step of it, for fp16 also its subnormal floor over t keys),
+    """|out - ref| from: each probability (with 8-bit blocks, times V's scale)
+    rounded once to the type (half a step of it, for fp16 also its subnormal
+    floor over t keys: 2^-25 of the largest such product, which with V's
+    largest code is V's row maximum, up to its scale's rounding),
     the output rounded once, fp32 sums (128 terms deep and t / 16 MFMA
     additions) and exponentials (2 ulp), and each score's own fp32 sum over
     head_dim products of magnitude mag in all, which moves a probability by
     as much in proportion, and their sum."""
-    pv = dtype if fmt == "16bit" else "bf16"
-    p = HALF_STEP[pv] * absv + (t * 2.0**-25 * vmax if pv == "f16" else 0.0)
+    p = HALF_STEP[dtype] * absv + (t * 2.0**-25 * vmax * 1.01 if dtype == "f16" else 0.0)
     fp32 = 2.0**-24 * (512 + t / 4 + 2 * 136 * mag[..., None]) * absv
     return (p + fp32) * (1 + HALF_STEP[dtype]) + HALF_STEP[dtype] * np.abs(ref) + TINY[dtype]
 

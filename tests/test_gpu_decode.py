@@ -207,6 +207,100 @@ def test_hidden_keys_do_not_arrive(sc, fmt, dtype, value, hq):
         pool.close()
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("lens,shared", [([200, 65, 1], 0), ([3, 40], 300), ([3, 40] * 4, 300)])
+def test_v_scales_of_any_size_in_fp16(sc, fmt, lens, shared):
+    """V rows whose scales differ by up to 2^24 between tokens, and for one
+    sequence are all near fp16's smallest number or largest: the probabilities
+    times the scale stay within fp16 all the same."""
+    from _decode_util import Pool, rand16
+    rng = np.random.default_rng(33)
+    hq, hkv, d, block = 8, 2, 64, 16
+    pool = Pool(sc, fmt, "f16", 1, hkv, d, block, 80)
+    try:
+        st = Step(sc, rng, pool, lens, 1, shared)
+        st.fill(rng, 0)
+
+        def rows(n, lo, hi):
+            x = rand16(rng, (n, hkv, d), "f16") * 2.0 ** rng.integers(lo, hi + 1, (n, hkv, 1))
+            return np.clip(x, -60000, 60000).astype(np.float16).astype(np.float64)
+        for lo, hi in ((-14, 10), (-14, -14), (13, 13)):
+            if shared:
+                st.sh = pool.write(st.shared_ids, 0, st.sh[0].astype(np.float16).astype(np.float64), rows(shared, lo, hi))
+            st.own = [pool.write(i, 0, given[0], rows(len(given[0]), lo, hi)) for i, given in zip(st.ids, st.given)]
+            q = rand16(rng, (len(lens), hq, d), "f16", 2.0)
+            out, lse = st.attend(0, q, hq)
+            st.check(q, hq, out, lse)
+    finally:
+        pool.close()
+
+
+@pytest.mark.parametrize("batch", [1, 4, 5, 8, 9, 16, 17, 32, 33, 64, 65])
+@pytest.mark.parametrize("fmt,dtype,d,shared", [
+    ("16bit", "bf16", 128, 1), ("16bit", "f16", 64, 127), ("int8", "bf16", 64, 129), ("e4m3", "bf16", 128, 600),
+    ("int8", "f16", 128, 257),
+])
+def test_rows_that_share_keys(sc, fmt, dtype, d, shared, batch):
+    """4 to 260 rows of a KV head over shared keys that end anywhere in a tile,
+    and a bad id in each place of the list: every row NaN, empty slots zero."""
+    from _decode_util import Pool, rand16
+    print("[shared]", fmt, dtype, d, shared, batch, flush=True)
+    rng = np.random.default_rng(batch + shared)
+    hq, hkv, block = 8, 2, 16
+    lens = [[1, 5, -1, 0][b % 4] for b in range(batch)]
+    pool = Pool(sc, fmt, dtype, 1, hkv, d, block, batch + shared // block + 4)
+    try:
+        st = Step(sc, rng, pool, lens, 1, shared)
+        st.fill(rng, 0)
+        q = rand16(rng, (batch, hq, d), dtype, 2.0)
+        out, lse = st.attend(0, q, hq)
+        st.check(q, hq, out, lse)
+        real = np.array(lens) >= 0
+        for at in sorted({0, len(st.shared_ids) // 2, len(st.shared_ids) - 1}):
+            st.d_shared[at] = [-1, 2**31 - 1, pool.blocks][at % 3]
+            out, lse = st.attend(0, q, hq)
+            assert np.isnan(out[real]).all() and np.isnan(lse[:, real]).all()
+            assert not out[~real].any() and np.all(lse[:, ~real] == -np.inf)
+            st.d_shared[at] = int(st.shared_ids[at])
+        out2, lse2 = st.attend(0, q, hq)
+        st.check(q, hq, out2, lse2)
+    finally:
+        pool.close()
+
+
+def test_a_row_of_one_key_is_its_value(sc):
+    """The most sequences a step may have, each with one key: its V row itself."""
+    import torch
+    from _decode_util import Pool, device16, host64, rand16
+    rng = np.random.default_rng(2)
+    n = 65536
+    pool = Pool(sc, "16bit", "bf16", 1, 1, 64, 1, 7)
+    try:
+        v = rand16(rng, (7, 1, 64), "bf16")
+        pool.write(range(7), 0, rand16(rng, (7, 1, 64), "bf16"), v)
+        ids = (np.arange(n) % 7).astype(np.int32)
+        table, lens = torch.from_numpy(ids).cuda(), torch.ones(n, dtype=torch.int32, device="cuda")
+        lens[5::11] = -1
+        q = device16(rand16(rng, (n, 2, 64), "bf16"), "bf16")
+        for top in (1, 1000):                # with and without partials
+            wide = table if top == 1 else torch.full((n, top), -1, dtype=torch.int32, device="cuda")
+            if top > 1:
+                wide[:, 0] = table
+            batch = sc.decode_batch(n, 1, top, top, wide.data_ptr(), lens.data_ptr(), 0, 0)
+            size = sc.sc_decode_workspace(pool.handle, batch, 2)
+            ws = torch.full((size + 1,), 0xFF, dtype=torch.uint8, device="cuda")
+            out = torch.full_like(q, 5.0)
+            torch.cuda.synchronize()
+            sc.sc_decode_attn(pool.handle, 0, batch, q.data_ptr(), 2, out.data_ptr(), ws.data_ptr(), size, 0, 0.0,
+                              stream())
+            torch.cuda.synchronize()
+            want = np.repeat(v[ids], 2, 1)
+            want[5::11] = 0
+            assert np.array_equal(host64(out), want)
+    finally:
+        pool.close()
+
+
 def test_peaky_and_masked_scores(sc):
     """Scores of thousands, keys that all score -infinity but one, and a row
     whose every score is -infinity (no maximum: NaN, as the formula has it)."""
