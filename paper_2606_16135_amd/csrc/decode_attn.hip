@@ -986,19 +986,21 @@ __global__ __launch_bounds__(kMergeThreads) void decode_merge_kernel(DecodeAttnA
   const int limit = len - a.batch.n_new + tok_in + 1;
   // The sequence's steps and, of the groups' runs, the first and the number
   // that touch them.
-  const int lane = threadIdx.x & 63;
-  int sum = 0;                               // steps of all sequences in this lane's stride
-  int begin = 0;                             // steps before each lane's row's sequence
   const int steps = steps_of<D, FMT>(len);
-  for (int b0 = 0; b0 < a.batch.batch; b0 += 64) {
-    const int s = b0 + lane < a.batch.batch ? steps_of<D, FMT>(own_len(a, b0 + lane)) : 0;
-    const int upto = wave_scan(s);
-    const int all = __builtin_amdgcn_readlane(upto, 63);
-    const int here = __shfl(upto - s, seq & 63);
-    if (seq >= b0 + 64) begin += all;
-    if (seq >= b0 && seq < b0 + 64) begin += here;
-    sum += all;
+  // One pass over the lengths for all rows of the wave (4096 sequences of 200 keys: 26 us; with a scan of every 64 57).
+  const int seq0 = __builtin_amdgcn_readfirstlane(seq);      // of its first row
+  int sum = 0, begin = 0;                    // steps of all sequences, and of those before
+  for (int b = threadIdx.x & 63; b < a.batch.batch; b += 64) {
+    const int s = steps_of<D, FMT>(own_len(a, b));
+    sum += s;
+    begin += b < seq0 ? s : 0;
   }
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    sum += __shfl_xor(sum, s);
+    begin += __shfl_xor(begin, s);
+  }
+  for (int b = seq0; b < seq; ++b) begin += steps_of<D, FMT>(own_len(a, b));   // a wave has 256 / D rows
   const int per = max(1, (sum + a.plan.groups - 1) / a.plan.groups);
   const int r0 = begin / per, own = steps > 0 ? (begin + steps - 1) / per - r0 + 1 : 0;
   const int shared = a.plan.shared_chunks;
