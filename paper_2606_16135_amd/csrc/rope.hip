@@ -17,6 +17,8 @@
 #include "sc_pool_view.h"
 #include "sc_quant.h"
 
+#include <algorithm>
+
 namespace sc {
 namespace {
 
@@ -190,10 +192,23 @@ hipError_t launch_rope(const RopeArgs &a, hipStream_t stream) {
   if (a.n_tokens <= 0 || a.heads[0] + a.heads[1] <= 0) return hipSuccess;
   // One token per workgroup while that leaves CUs idle, else one angle per thread.
   const int per = a.n_tokens <= 1024 ? 1 : kTokens;
-  const unsigned groups = (unsigned)(((int64_t)a.n_tokens + per - 1) / per);
-  hipLaunchKernelGGL(a.dtype == SC_DTYPE_BF16 ? rope_kernel<SC_DTYPE_BF16> : rope_kernel<SC_DTYPE_F16>, dim3(groups),
-                     dim3(kThreads), 0, stream, a, per, uq, uk);
-  return hipGetLastError();
+  // A launch's threads are counted in 32 bits.
+  constexpr int64_t kSlice = 1 << 25;
+  for (int64_t t0 = 0; t0 < a.n_tokens; t0 += kSlice) {
+    RopeArgs b = a;
+    b.n_tokens = (int32_t)std::min(kSlice, a.n_tokens - t0);
+    b.positions += t0;
+    for (int i = 0; i < 2; ++i) {
+      if (b.heads[i] == 0) continue;
+      b.x[i] += t0 * b.x_stride[i];
+      b.y[i] += t0 * b.y_stride[i];
+    }
+    hipLaunchKernelGGL(a.dtype == SC_DTYPE_BF16 ? rope_kernel<SC_DTYPE_BF16> : rope_kernel<SC_DTYPE_F16>,
+                       dim3((unsigned)((b.n_tokens + per - 1) / per)), dim3(kThreads), 0, stream, b, per, uq, uk);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_decode_store(const DecodeStoreArgs &a, hipStream_t stream) {

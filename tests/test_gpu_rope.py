@@ -138,3 +138,27 @@ def test_nan_and_infinity_stay_in_their_pair(sc):
     bad = sorted(torch.nonzero(~torch.isfinite(y[0, 0])).flatten().tolist())
     assert bad == [5, 8, 37, 40]
     sc.sc_rope_destroy(rope)
+
+
+def test_more_tokens_than_one_launch_takes(sc):
+    """2^26 + 9 tokens in place (8.6 GB), checked around the launches' ends."""
+    import torch
+    from _decode_util import device16, host64, rand16
+    t = 2**26 + 9
+    rng = np.random.default_rng(1)
+    rope = sc.sc_rope_create(64, 64)
+    x = torch.zeros((t, 1, 64), dtype=torch.bfloat16, device="cuda")
+    p = torch.arange(t, dtype=torch.int32, device="cuda")
+    at = np.concatenate([np.arange(a - 9, a + 9) for a in (9, 2**24, 2**25, 2**26)])
+    rows = rand16(rng, (len(at), 1, 64), "bf16")
+    x[torch.from_numpy(at).cuda()] = device16(rows, "bf16")
+    torch.cuda.synchronize()
+    sc.sc_rope_apply(rope, 0, t, p.data_ptr(), 0, 0, 0, 0, 0, x.data_ptr(), 64, 1, x.data_ptr(), 64,
+                     torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    sc.sc_rope_destroy(rope)
+    theta = od.frequencies(64, 10000.0)
+    ref = od.rotate(rows, at, theta, "half")
+    y = host64(x[torch.from_numpy(at).cuda()])
+    assert np.all(np.abs(y - ref) <= bound(rows, ref, theta, "half", "bf16", 1.0, at))
+    assert torch.count_nonzero(x[2**25 + 9:2**26 - 9]) == 0
