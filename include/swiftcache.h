@@ -593,7 +593,9 @@ sc_status sc_rope_apply(const sc_rope *rope, int32_t dtype, int64_t n_tokens, co
  * block_size, or an id it needs is outside the pool or not lent; that is
  * only known on the device, where nothing outside the pool is touched:
  * sc_decode_store skips the token, sc_decode_attn gives the sequence's rows
- * (a bad shared id: all rows) NaN.
+ * (a bad shared id: all rows) NaN.  Which HBM blocks are lent is taken when
+ * the call is made: a captured step must not be replayed after
+ * sc_pool_resize has released blocks that its lists name.
  */
 typedef struct {
   int32_t batch;
@@ -649,8 +651,9 @@ sc_status sc_decode_workspace(const sc_pool *pool, const sc_decode_batch *batch,
  * that may overlap, and captured graphs, need workspaces of their own.
  * Errors: SC_ERR_INVALID (null, misaligned, sizes outside their ranges, a
  * workspace too small), SC_ERR_UNSUPPORTED (GQA group > 16), SC_ERR_RANGE
- * (layer; more than 65536 sequences, 2^31 - 1 rows, 2^31 - 257 shared or own
- * tokens, or 2^30 steps of 64 or 32 keys over all sequences at max_len).
+ * (layer; more than 65536 sequences, 2^31 - 1 rows, 2^31 - 2^18 shared and own
+ * tokens, 2^30 steps of 64 or 32 keys over all sequences at max_len, or 2^22
+ * pairs of a sequence's 16 rows and a KV head).
  */
 sc_status sc_decode_attn(sc_pool *pool, int32_t layer, const sc_decode_batch *batch, const void *q,
                          int32_t n_q_heads, float scale, void *out, float *lse, void *workspace,

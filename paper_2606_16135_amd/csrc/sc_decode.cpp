@@ -90,7 +90,8 @@ sc_status check_batch(const sc_pool *pool, const sc_decode_batch *b, bool pointe
     return fail(SC_ERR_INVALID, "decode batch: batch %d, n_new %d (1..16), max_blocks %d, max_len %d, shared_len %d",
                 b->batch, b->n_new, b->max_blocks, b->max_len, b->shared_len);
   if (b->batch > 65536) return fail(SC_ERR_RANGE, "a decode step of %d sequences (at most 65536)", b->batch);
-  if ((int64_t)b->max_len + b->shared_len > INT32_MAX - 257)
+  // The kernels add to a position in 32 bits: up to three tiles, and the rounding of every chunk.
+  if ((int64_t)b->max_len + b->shared_len > INT32_MAX - (1 << 18))
     return fail(SC_ERR_RANGE, "%d shared and %d own tokens exceed 32-bit positions", b->shared_len, b->max_len);
   if (!pointers) return SC_OK;
   if (!b->kv_len || (b->max_blocks > 0 && !b->block_ids) || (b->shared_len > 0 && !b->shared_ids))
@@ -114,7 +115,7 @@ constexpr int kDecodeCus = 256;              // MI355X
 constexpr int kNarrowRows = 16;
 // Waves that read own keys: two per SIMD, what a CU holds of them.
 constexpr int kDecodeWaves = 8 * kDecodeCus;
-constexpr int kMaxDecodeGroups = 1 << 23;    // workgroups of a launch
+constexpr int kMaxDecodeGroups = 1 << 22;    // workgroups of a launch, whose threads are counted in 32 bits
 // The wide part's tile of rows and keys, and the times a CU takes for one,
 // measured: 256 rows 5.3 us (64 x 4 rows of 5 heads over 32768 bf16 keys),
 // few rows 2.5 us (the tile's loads); and what a CU reads of own keys.

@@ -102,6 +102,61 @@ class Step:
             assert np.all(le <= lb), (b, float((le / lb).max()))
 
 
+def test_first_call_of_a_kernel_made_in_a_capture(sc):
+    """Steps captured before the process has launched their kernels, over the
+    largest LDS use among them; the replays equal the eager call."""
+    import torch
+    from _decode_util import Pool, device16, rand16
+    rng = np.random.default_rng(17)
+    pool = Pool(sc, "e4m3", "bf16", 1, 2, 64, 16, 40)
+    try:
+        st = Step(sc, rng, pool, [5, 30, 1] * 4, 1, 200)
+        st.fill(rng, 0)
+        q = device16(rand16(rng, (12, 8, 64), "bf16"), "bf16")
+        n = sc.sc_decode_workspace(pool.handle, st.batch, 8)
+        ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+        out = torch.zeros_like(q)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            sc.sc_decode_attn(pool.handle, 0, st.batch, q.data_ptr(), 8, out.data_ptr(), ws.data_ptr(), n,
+                              stream=stream())
+        want = None
+        for _ in range(3):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            got = out.clone()
+            eager, lse = st.attend(0, q, 8)
+            st.check(q.double().cpu().numpy(), 8, eager, lse)
+            assert np.array_equal(got.double().cpu().numpy(), eager)
+            assert want is None or torch.equal(got, want)
+            want = got
+    finally:
+        pool.close()
+
+
+@pytest.mark.parametrize("fmt", ["16bit", "e4m3"])
+def test_steps_without_own_keys(sc, fmt):
+    """max_len and max_blocks of 0: only the shared keys, or none at all."""
+    import torch
+    from _decode_util import Pool, rand16
+    rng = np.random.default_rng(4)
+    pool = Pool(sc, fmt, "f16", 1, 2, 64, 16, 8)
+    try:
+        for shared in (0, 1, 70):
+            st = Step(sc, rng, pool, [0, -1, 0, 0, 0], 1, shared)
+            st.fill(rng, 0)
+            st.batch = sc.decode_batch(5, 1, 0, 0, 0, st.d_len.data_ptr(), st.d_shared.data_ptr() if shared else 0,
+                                       shared)
+            q = rand16(rng, (5, 8, 64), "f16")
+            out, lse = st.attend(0, q, 8)
+            st.check(q, 8, out, lse)
+            assert torch.isfinite(torch.from_numpy(out)).all()
+    finally:
+        pool.close()
+
+
 CASES = [
     # fmt, type, head_dim, q heads, KV heads, block, lengths, new, shared
     ("16bit", "bf16", 128, 8, 2, 16, [1], 1, 0),

@@ -93,6 +93,7 @@ BATCHES = [
     (dict(batch=0), "INVALID"), (dict(batch=-1), "INVALID"), (dict(n_new=0), "INVALID"), (dict(n_new=17), "INVALID"),
     (dict(max_blocks=-1), "INVALID"), (dict(max_len=-1), "INVALID"), (dict(shared_len=-1), "INVALID"),
     (dict(batch=65537), "RANGE"), (dict(max_len=2**31 - 257), "RANGE"),
+    (dict(max_len=2**31 - 2**18), "RANGE"), (dict(max_len=1, shared_len=2**31 - 2**18 - 1), "RANGE"),
     (dict(max_len=2**30, shared_len=2**30), "RANGE"),
 ]
 POINTERS = [dict(kv_len=0), dict(block_ids=0), dict(shared_len=5, shared_ids=0), dict(kv_len=FAKE + 2),
