@@ -594,6 +594,11 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int64_t fir
 // barrier a tile: while tile t is computed, tile t + 1 goes from the loaders'
 // registers into the other buffer (waves 0-3 load and lay out V, waves 4-7 K)
 // and tile t + 2 is loaded.  LDS holds whole MFMA operands, 16 bytes a lane.
+// The two waves of a SIMD (w and w + 4) do their part of that at the opposite
+// ends of a tile, so that one takes products while the other is at its
+// softmax: 64 x 4 rows of 5 heads over 32768 int8 keys take 246 us (0.70
+// PFLOP/s); with both in the middle of a tile, in step from barrier to
+// barrier, 275 us.
 //
 // The vector unit is the bound (per score half a maximum, an FMA, an
 // exponential, an add and half a pack, for 8-bit blocks a multiplication by
@@ -756,9 +761,9 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
     }
   };
 
-  RowState st[2] = {{kNegInf, 0.f}, {kNegInf, 0.f}};
+  float l[2] = {0.f, 0.f};
   float neg_ref[2] = {0.f, 0.f};             // -m, or 0 while there is none
-  float limit[2] = {kNegInf, kNegInf};       // a score above it moves m
+  float limit[2] = {kNegInf, kNegInf};       // a score this much above m moves it; -infinity: no m yet
   f32x4 o[2][G::kVd];
 #pragma unroll
   for (int r = 0; r < 2; ++r)
@@ -805,32 +810,33 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
     u32x4 pf[2];
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      float x[8];
+      float x[8], y[8];                      // scores less the reference; y: with V's scale's part
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float y = s[r][i >> 2][i & 3];
-        if constexpr (weigh_scales<D, FMT, DT>()) x[i] = __builtin_fmaf(y, ks[i >> 2][i & 3], lv[i >> 2][i & 3]);
-        else x[i] = G::k8 ? y * ks[i >> 2][i & 3] : y;
+        x[i] = __builtin_fmaf(s[r][i >> 2][i & 3], ks[i >> 2][i & 3], neg_ref[r]);
+        y[i] = weigh_scales<D, FMT, DT>() ? x[i] + lv[i >> 2][i & 3] : x[i];
       }
-      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if constexpr (!G::k8) top *= a.scale_log2;
+      float top = fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
       if (wave_any(top > limit[r])) {        // a new reference for the rows that need one
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float m = fmaxf(st[r].m, top);
-        const float alpha = __builtin_amdgcn_exp2f(st[r].m - m);   // m is finite or +infinity here, or both are -infinity
-        const float f = m == kNegInf ? 1.f : alpha;
-        st[r].m = m;
-        st[r].l *= f;
-        limit[r] = m + kRefSlack;
-        neg_ref[r] = m == kNegInf ? 0.f : -m;
+        // (there may be none yet, nothing to scale then, and none stays none
+        // while all scores are -infinity)
+        const bool none = limit[r] == kNegInf;
+        const float up = none ? (top == kNegInf ? 0.f : top) : fmaxf(top, 0.f);
+        const float f = none ? 1.f : __builtin_amdgcn_exp2f(-up);
+        if (top != kNegInf) limit[r] = kRefSlack;
+        neg_ref[r] -= up;
+        l[r] *= f;
 #pragma unroll
         for (int d = 0; d < G::kVd; ++d) o[r][d] *= f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] -= up;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i >> 2][i & 3], ks[i >> 2][i & 3], neg_ref[r]));
-        st[r].l += x[i];
+        x[i] = __builtin_amdgcn_exp2f(x[i]);
+        l[r] += x[i];
       }
       if constexpr (G::k8) {
 #pragma unroll
@@ -850,7 +856,6 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   // Tile t is addressed in iteration t - 3, loaded in t - 2, written in t - 1;
   // its address slot and its bad flag are those of its parity, and a barrier
   // lies between every use by one tile and the next one's.
-  auto mine = [&](int u) { return (u & (key_waves - 1)) == key_wave; };
   int end = tiles;                           // tiles before the first bad id
   auto check = [&](int t) {
     if (t < end && lds.bad[t & 1] != 0) end = t;
@@ -874,15 +879,16 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
     __syncthreads();
     check(2);
   }
-  for (int t = 0; t < end; ++t) {
-    if (t + 3 < end) fetch_id(t + 3);
-    if (mine(0)) compute(t, 0);
-    if (mine(1)) compute(t, 1);
+  auto move = [&](int t) {                   // the next tile into LDS and the one after it into the registers
     if (t + 1 < end) write_tile(t + 1);
     my_scale = next_scale;
     if (t + 2 < end) load_tile(t + 2);
-    if (mine(2)) compute(t, 2);
-    if (mine(3)) compute(t, 3);
+  };
+  for (int t = 0; t < end; ++t) {
+    if (t + 3 < end) fetch_id(t + 3);
+    if (!loads_v) move(t);
+    for (int u = key_wave; u < 4; u += key_waves) compute(t, u);
+    if (loads_v) move(t);
     if (t + 3 < end) take_addr(t + 3);
     __syncthreads();
     check(t + 3);
@@ -899,9 +905,10 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
   static_assert(sizeof(lds.k) + sizeof(lds.v) >= kWideWaves * 16 * kJoinRow * sizeof(float), "one half of the rows");
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    float l = st[r].l;
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
+    float sum_l = l[r];
+    sum_l += __shfl_xor(sum_l, 16);
+    sum_l += __shfl_xor(sum_l, 32);
+    const float m = limit[r] == kNegInf ? kNegInf : -neg_ref[r];
     if (key_waves == 1) {
       if (!has_row[r]) continue;
       const int64_t at = (int64_t)chunk * all_rows + out_row[r];
@@ -912,7 +919,7 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
         for (int d = 0; d < G::kVd; ++d) v[d] = o[r][d][i];
         store_f32(a.part_o + at * D + G::kVd * (4 * g + i), v);
       }
-      if (g == 0) a.part_ml[at] = bad ? float2{nan, nan} : float2{st[r].m, l};
+      if (g == 0) a.part_ml[at] = bad ? float2{nan, nan} : float2{m, sum_l};
       continue;
     }
     if (r == 1) __syncthreads();             // the first half of the rows has been read
@@ -923,16 +930,16 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
       for (int d = 0; d < G::kVd; ++d) v[d] = o[r][d][i];
       store_f32(join_o + (wave * 16 + n) * kJoinRow + G::kVd * (4 * g + i), v);
     }
-    if (g == 0) join_ml[wave * 16 + n] = float2{st[r].m, l};
+    if (g == 0) join_ml[wave * 16 + n] = float2{m, sum_l};
     __syncthreads();
     // Thread: 4 dims of one of the 16 row_waves rows.
     for (int idx = tid; idx < row_waves * 16 * (D / 4); idx += 64 * kWideWaves) {
       const int jr = idx / (D / 4), d0 = 4 * (idx % (D / 4));          // jr = 16 * row wave + row
       const int row = tile * kWideRows + (jr >> 4) * 32 + 16 * r + (jr & 15);
       if (row >= rows) continue;
-      float m = kNegInf, sum = 0.f;
-      for (int w = 0; w < key_waves; ++w) m = fmaxf(m, join_ml[w * row_waves * 16 + jr].x);
-      const float ref = m == kNegInf ? 0.f : m;
+      float top = kNegInf, sum = 0.f;
+      for (int w = 0; w < key_waves; ++w) top = fmaxf(top, join_ml[w * row_waves * 16 + jr].x);
+      const float ref = top == kNegInf ? 0.f : top;
       f32x4 v = {0.f, 0.f, 0.f, 0.f};
       for (int w = 0; w < key_waves; ++w) {
         const float2 ml = join_ml[w * row_waves * 16 + jr];
@@ -943,7 +950,7 @@ __device__ __forceinline__ void wide_body(const DecodeAttnArgs &a, int id, int r
       const int token = row / group;
       const int64_t at = (int64_t)chunk * all_rows + (int64_t)token * a.n_q_heads + kvh * group + (row - token * group);
       *reinterpret_cast<f32x4 *>(a.part_o + at * D + d0) = v;
-      if (d0 == 0) a.part_ml[at] = bad ? float2{nan, nan} : float2{m, sum};
+      if (d0 == 0) a.part_ml[at] = bad ? float2{nan, nan} : float2{top, sum};
     }
   }
 }

@@ -117,10 +117,10 @@ constexpr int kNarrowRows = 16;
 constexpr int kDecodeWaves = 8 * kDecodeCus;
 constexpr int kMaxDecodeGroups = 1 << 22;    // workgroups of a launch, whose threads are counted in 32 bits
 // The wide part's tile of rows and keys, and the times a CU takes for one,
-// measured: 256 rows 5.3 us (64 x 4 rows of 5 heads over 32768 bf16 keys),
+// measured: 256 rows 4.8 us (64 x 4 rows of 5 heads over 32768 int8 keys),
 // few rows 2.5 us (the tile's loads); and what a CU reads of own keys.
 constexpr int kWideRows = 256, kWideKeys = 128;
-constexpr double kWideTileUs = 2.5, kWideRowUs = 5.7 / 256, kCuBytesPerUs = 22e3;
+constexpr double kWideTileUs = 2.5, kWideRowUs = 4.8 / 256, kCuBytesPerUs = 22e3;
 // From a workgroup's start to its first tile; writing and reading partials.
 constexpr double kStartUs = 8, kPartBytesPerUs = 4e6;
 constexpr int64_t kMinOwnCus = 32;
