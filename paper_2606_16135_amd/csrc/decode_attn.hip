@@ -8,8 +8,9 @@
 // over the shared keys and the row's own.  A row's keys are cut into chunks;
 // every chunk gives a partial (maximum m, sum l = sum 2^(s_j - m), O = sum
 // 2^(s_j - m) v_j, all fp32) and decode_merge_kernel joins them: with M the
-// largest m, o = sum 2^(m - M) O / sum 2^(m - M) l.  One chunk in all and no
-// shared prefix: the first kernel writes the result itself.
+// largest m, o = sum 2^(m - M) O / sum 2^(m - M) l.  Short sequences and no
+// shared prefix: the first kernel writes the result itself, a wave alone or
+// the waves of a workgroup joined in LDS.
 //
 // Narrow (narrow_body): up to 16 rows of one KV head (the tokens and query
 // heads of one sequence) against one chunk, bound by reading K and V once:
@@ -268,10 +269,18 @@ struct NarrowLds {                           // of one wave
   float scale[3][64];                        // K, V, log_scale(V)
 };
 
-// Keys [k0, k1) of sequence `seq`, as partial `part` of its rows.
+// A wave's partials that its workgroup joins in LDS.
+template <int D>
+struct JoinLds {
+  float o[16][D + 4];                        // padded against bank conflicts
+  float2 ml[16];
+};
+
+// Keys [k0, k1) of sequence `seq`, as partial `part` of its rows (`join`:
+// the partial goes there instead).
 template <int D, int FMT, int DT, bool SHARED>
 __device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, int len, int k0, int k1, int kvh, int tile,
-                                            int64_t part, NarrowLds &lds) {
+                                            int64_t part, NarrowLds &lds, JoinLds<D> *join = nullptr) {
   using G = Geo<D, FMT>;
   constexpr int kStep = G::kStep, kTiles = kStep / 16, kHalves = kStep / 32;
   const PoolView &p = a.pool;
@@ -485,17 +494,18 @@ __device__ __forceinline__ void narrow_keys(const DecodeAttnArgs &a, int seq, in
   if (!has_row) return;
   if (bad) st.m = st.l = __builtin_nanf("");
   // o[d][i]: dim G::kVd * (4 g + i) + d of row n.
-  if (SHARED || !a.plan.direct) {
+  if (SHARED || join != nullptr || !a.plan.direct) {
     // `part` is the partial's first row; rows follow tokens, then heads.
     const int64_t at = part + (int64_t)(SHARED ? token : tok_in) * a.n_q_heads + head;
+    float *const to = join != nullptr ? join->o[n] : a.part_o + at * D;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float v[G::kVd];
 #pragma unroll
       for (int d = 0; d < G::kVd; ++d) v[d] = o[d][i];
-      store_f32(a.part_o + at * D + G::kVd * (4 * g + i), v);
+      store_f32(to + G::kVd * (4 * g + i), v);
     }
-    if (g == 0) a.part_ml[at] = float2{st.m, st.l};
+    if (g == 0) *(join != nullptr ? &join->ml[n] : a.part_ml + at) = float2{st.m, st.l};
     return;
   }
   const int64_t out_row = (int64_t)token * a.n_q_heads + head;
@@ -586,6 +596,51 @@ __device__ __forceinline__ void narrow_body(const DecodeAttnArgs &a, int64_t fir
       }
       before += __builtin_amdgcn_readlane(upto, 63);
     }
+  }
+}
+
+// Short sequences (DecodePlan::joined): workgroup `id` takes 16 rows of one KV
+// head of a sequence, its waves equal runs of its steps, and joins them in
+// LDS: no partials in memory and no second launch.
+template <int D, int FMT, int DT>
+__device__ __forceinline__ void joined_body(const DecodeAttnArgs &a, int id, int row_tiles, char *smem) {
+  constexpr int kStep = Geo<D, FMT>::kStep;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  JoinLds<D> *const join = reinterpret_cast<JoinLds<D> *>(smem + kWaves * sizeof(NarrowLds));
+  const int kvh = id % a.pool.n_kv_heads;
+  id /= a.pool.n_kv_heads;
+  const int tile = id % row_tiles, seq = id / row_tiles;
+  const int len = own_len(a, seq);
+  const int run = (steps_of<D, FMT>(len) + kWaves - 1) / kWaves * kStep;
+  narrow_keys<D, FMT, DT, false>(a, seq, len, wave * run, min(max(len, 0), (wave + 1) * run), kvh, tile, 0,
+                                 reinterpret_cast<NarrowLds *>(smem)[wave], join + wave);
+  __syncthreads();
+  const int group = a.plan.group, n_new = a.batch.n_new;
+  // Thread: 4 dims of a row.
+  for (int idx = threadIdx.x; idx < 16 * (D / 4); idx += 64 * kWaves) {
+    const int r = idx / (D / 4), d0 = 4 * (idx % (D / 4)), row = tile * 16 + r;
+    if (row >= n_new * group) break;
+    const int tok_in = row / group, token = seq * n_new + tok_in, head = kvh * group + row - tok_in * group;
+    float m = kNegInf, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, join[w].ml[r].x);
+    const float ref = m == kNegInf ? 0.f : m;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float2 ml = join[w].ml[r];
+      const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+      l += f * ml.y;
+      o += f * *reinterpret_cast<const f32x4 *>(&join[w].o[r][d0]);
+    }
+    const bool none = len != kBad && len - n_new + tok_in + 1 <= 0;   // no key at all: zeros
+    const float inv = 1.f / l;
+    u32x2 v;
+    v.x = none ? 0u : pack16<DT>(o[0] * inv, o[1] * inv);
+    v.y = none ? 0u : pack16<DT>(o[2] * inv, o[3] * inv);
+    *reinterpret_cast<u32x2 *>(a.out + ((int64_t)token * a.n_q_heads + head) * D + d0) = v;
+    if (d0 == 0 && a.lse != nullptr)
+      a.lse[(int64_t)head * a.plan.tokens + token] = none ? kNegInf : (m + __builtin_log2f(l)) * 0.6931471805599453f;
   }
 }
 
@@ -968,6 +1023,8 @@ __global__ __launch_bounds__(64 * (WIDE ? kWideWaves : kWaves), 2) void decode_a
   constexpr int kGroupWaves = WIDE ? kWideWaves : kWaves;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int id = blockIdx.x;
+  if constexpr (!WIDE)
+    if (a.plan.joined) return joined_body<D, FMT, DT>(a, id, own_tiles, smem);
   if (id >= shared_groups)
     narrow_body<D, FMT, DT, false>(a, (int64_t)(id - shared_groups) * kGroupWaves, own_tiles, smem);
   else if constexpr (WIDE)
@@ -1080,8 +1137,8 @@ template <int D, int FMT, int DT, bool WIDE>
 hipError_t launch_chunks(const DecodeAttnArgs &a, hipStream_t stream) {
   const DecodePlan &pl = a.plan;
   constexpr int waves = WIDE ? kWideWaves : kWaves;
-  constexpr size_t lds = WIDE ? sizeof(WideLds<D>) : waves * sizeof(NarrowLds);
-  static_assert(lds >= waves * sizeof(NarrowLds), "both bodies' LDS");
+  static_assert(sizeof(WideLds<D>) >= kWideWaves * sizeof(NarrowLds), "both bodies' LDS");
+  const size_t lds = WIDE ? sizeof(WideLds<D>) : waves * (sizeof(NarrowLds) + (pl.joined ? sizeof(JoinLds<D>) : 0));
   const void *kernel = reinterpret_cast<const void *>(&decode_attn_kernel<D, FMT, DT, WIDE>);
   if (lds > 64 * 1024) {
     static std::atomic<uint64_t> ready{0};   // devices on which the kernel may use that much LDS
@@ -1102,7 +1159,9 @@ hipError_t launch_chunks(const DecodeAttnArgs &a, hipStream_t stream) {
   auto narrow_groups = [&](int64_t units) { return (units * heads + waves - 1) / waves; };
   const int shared_groups = WIDE ? heads * shared_tiles * pl.shared_chunks
                                  : (int)narrow_groups((int64_t)shared_tiles * pl.shared_chunks);
-  const int64_t groups = shared_groups + narrow_groups((int64_t)own_tiles * (pl.direct ? a.batch.batch : pl.groups));
+  const int64_t groups =
+      pl.joined ? (int64_t)heads * own_tiles * a.batch.batch
+                : shared_groups + narrow_groups((int64_t)own_tiles * (pl.direct ? a.batch.batch : pl.groups));
   hipLaunchKernelGGL((decode_attn_kernel<D, FMT, DT, WIDE>), dim3((unsigned)groups), dim3(64 * waves), lds, stream, a,
                      shared_groups, shared_tiles, own_tiles);
   return hipGetLastError();
@@ -1113,7 +1172,7 @@ hipError_t launch_all(const DecodeAttnArgs &a, hipStream_t stream) {
   const DecodePlan &pl = a.plan;
   const hipError_t e = pl.shared_wide && pl.shared_chunks > 0 ? launch_chunks<D, FMT, DT, true>(a, stream)
                                                               : launch_chunks<D, FMT, DT, false>(a, stream);
-  if (e != hipSuccess || pl.direct) return e;
+  if (e != hipSuccess || pl.direct || pl.joined) return e;
   // A row's partials: all shared chunks, and the own keys' share of the groups
   // if the sequences were equally long (the rows of longer ones loop).
   const int parts = pl.shared_chunks + (pl.groups + a.batch.batch - 1) / a.batch.batch;

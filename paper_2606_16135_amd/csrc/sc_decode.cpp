@@ -116,6 +116,13 @@ constexpr int kNarrowRows = 16;
 // Waves that read own keys: two per SIMD, what a CU holds of them.
 constexpr int kDecodeWaves = 8 * kDecodeCus;
 constexpr int kMaxDecodeGroups = 1 << 22;    // workgroups of a launch, whose threads are counted in 32 bits
+// Steps of the longest sequence up to which a workgroup takes a sequence alone
+// and joins its waves in LDS, instead of waves taking equal runs of all
+// sequences and a second launch merging them.  32 / 8 heads of 128, 16-bit,
+// joined against apart: 1 sequence of 400 keys 7.4 against 6.0 + 4.5 us, of
+// 700 10.0 against 6.0 + 4.4, of 1000 12.8 against 6.4 + 5.2; 32 sequences of
+// 700 20.1 against 20.1 + 4.8; 8 of 1000 18.7 against 12.8 + 4.6.
+constexpr int kJoinedSteps = 24;
 // The wide part's tile of rows and keys, and the times a CU takes for one,
 // measured: 256 rows 4.8 us (64 x 4 rows of 5 heads over 32768 int8 keys),
 // few rows 2.5 us (the tile's loads); and what a CU reads of own keys.
@@ -184,7 +191,8 @@ sc_status plan_decode(const sc_pool *pool, const sc_decode_batch *b, int hq, Dec
     return fail(SC_ERR_RANGE, "%d sequences of up to %d tokens are too many keys for a decode step", b->batch, b->max_len);
   p.groups = (int32_t)std::max<int64_t>(1, std::min<int64_t>(own_waves / heads, steps));
   p.direct = b->shared_len == 0 && b->max_len <= step;
-  if (heads * std::max<int64_t>(p.groups, p.direct ? b->batch : 0) > kMaxDecodeGroups || shared_items > kMaxDecodeGroups ||
+  p.joined = b->shared_len == 0 && !p.direct && b->max_len <= kJoinedSteps * step;
+  if (heads * std::max<int64_t>(p.groups, p.direct || p.joined ? b->batch : 0) > kMaxDecodeGroups || shared_items > kMaxDecodeGroups ||
       (all_rows + 15) / 16 * hkv > kMaxDecodeGroups)
     return fail(SC_ERR_RANGE, "a decode step of %d sequences x %d KV heads needs too many workgroups", b->batch, hkv);
   *out = p;
@@ -195,7 +203,7 @@ sc_status plan_decode(const sc_pool *pool, const sc_decode_batch *b, int hq, Dec
 size_t workspace_bytes_of(const DecodePlan &p, const sc_decode_batch *b, int hq, int head_dim, size_t *ml_off) {
   const size_t seq_rows = (size_t)b->n_new * hq;
   const size_t rows =
-      p.direct ? 0 : (size_t)p.shared_chunks * b->batch * seq_rows + ((size_t)p.groups + b->batch) * seq_rows;
+      p.direct || p.joined ? 0 : (size_t)p.shared_chunks * b->batch * seq_rows + ((size_t)p.groups + b->batch) * seq_rows;
   *ml_off = rows * head_dim * sizeof(float);
   return *ml_off + rows * sizeof(float2);
 }

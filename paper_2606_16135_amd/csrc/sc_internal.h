@@ -204,6 +204,7 @@ struct DecodePlan {
   int32_t shared_chunk, shared_chunks;
   int32_t shared_wide;        // the shared keys by the kernel for more than 16 rows
   int32_t direct;             // no shared prefix and one step a sequence: one group each, no partials
+  int32_t joined;             // no shared prefix and few steps a sequence: a workgroup each, partials in LDS only
 };
 struct DecodeAttnArgs {
   PoolView pool;

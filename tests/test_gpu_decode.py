@@ -171,6 +171,9 @@ CASES = [
     ("int8", "bf16", 64, 15, 3, 16, [65, 127, 128], 3, 0),
     ("e4m3", "f16", 128, 32, 2, 32, [1, 900], 2, 0),
     ("16bit", "f16", 128, 32, 2, 16, [257, 64], 16, 0),
+    ("16bit", "bf16", 128, 8, 2, 16, [768, 33, 0, -1, 97, 128, 32, 1], 1, 0),
+    ("16bit", "f16", 64, 12, 2, 32, [1536, 5, 2, 260], 4, 0),
+    ("e4m3", "bf16", 128, 8, 8, 16, [1536, 64, 65, 256, 257], 1, 0),
     ("16bit", "bf16", 128, 8, 8, 16, [5], 1, 100),
     ("int8", "f16", 64, 8, 2, 16, [5, 0, -1, 300], 1, 1),
     ("e4m3", "bf16", 128, 4, 2, 16, [33, 1], 3, 700),
@@ -426,6 +429,33 @@ def test_bad_lists_give_nan_rows_and_touch_nothing(sc, fmt, shared):
             st.d_shared[shared // 16 // 2] = 2**31 - 1
             out, _ = st.attend(0, q, 8)
             assert np.isnan(out[:2]).all() and not out[2:].any()
+    finally:
+        pool.close()
+
+
+def test_bad_lists_of_long_steps(sc):
+    """As above, with a bound on the lengths that makes partials of own keys."""
+    from _decode_util import Pool, rand16
+    rng = np.random.default_rng(5)
+    pool = Pool(sc, "16bit", "f16", 1, 2, 64, 16, 200)
+    try:
+        lens = [900, 50, 1200, 30, -1, 64]
+        st = Step(sc, rng, pool, lens, 1, 0, max_len=2000, extra=60, ids=rng.permutation(150))
+        st.fill(rng, 0)
+        q = rand16(rng, (6, 8, 64), "f16")
+        good, lse = st.attend(0, q, 8)
+        st.check(q, 8, good, lse)
+        st.d_table[0, 56] = 200               # the last block of a long list, the middle of another
+        st.d_table[2, 40] = -1
+        st.d_len[5] = 2001
+        out, lse = st.attend(0, q, 8)
+        for b in (0, 2, 5):
+            assert np.isnan(out[b]).all() and np.isnan(lse[:, b]).all(), b
+        st.d_len[5] = 64
+        out, lse = st.attend(0, q, 8)
+        for b in (1, 3, 4, 5):
+            assert np.array_equal(out[b], good[b]), b
+        assert np.isnan(out[[0, 2]]).all()
     finally:
         pool.close()
 

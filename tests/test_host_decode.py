@@ -153,8 +153,10 @@ def test_workspace_grows_with_the_batch_and_is_nothing_for_one_chunk(sc, pool):
     assert sc.sc_decode_workspace(p, batch_of(sc, max_len=32), 32) == 0
     assert sc.sc_decode_workspace(p, batch_of(sc, max_len=0, max_blocks=0), 32) == 0
     row = 32 * (128 * 4 + 8)                      # one sequence's partials
-    # two sequences of up to two steps: four groups of waves, a partial per group and sequence boundary
-    assert sc.sc_decode_workspace(p, batch_of(sc, max_len=64), 32) == (4 + 2) * row
+    # short sequences, joined within their workgroup
+    assert sc.sc_decode_workspace(p, batch_of(sc, max_len=24 * 32), 32) == 0
+    # two sequences of up to 25 steps: 50 groups of waves, a partial per group and sequence boundary
+    assert sc.sc_decode_workspace(p, batch_of(sc, max_len=24 * 32 + 1), 32) == (50 + 2) * row
     # long ones: what the device holds, 2048 waves over 8 KV heads
     assert sc.sc_decode_workspace(p, batch_of(sc, batch=1, max_len=50000), 32) == (256 + 1) * row
     # with a shared prefix: its chunk's partials of both sequences too
