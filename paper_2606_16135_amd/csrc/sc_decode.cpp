@@ -121,7 +121,9 @@ constexpr int kMaxDecodeGroups = 1 << 22;    // workgroups of a launch, whose th
 // sequences and a second launch merging them.  32 / 8 heads of 128, 16-bit,
 // joined against apart: 1 sequence of 400 keys 7.4 against 6.0 + 4.5 us, of
 // 700 10.0 against 6.0 + 4.4, of 1000 12.8 against 6.4 + 5.2; 32 sequences of
-// 700 20.1 against 20.1 + 4.8; 8 of 1000 18.7 against 12.8 + 4.6.
+// 700 20.1 against 20.1 + 4.8; 8 of 1000 18.7 against 12.8 + 4.6.  (What bounds
+// it is what one CU reads, 22 to 35 KB a us: eight waves instead of four take
+// as long.)
 constexpr int kJoinedSteps = 24;
 // The wide part's tile of rows and keys, and the times a CU takes for one,
 // measured: 256 rows 4.8 us (64 x 4 rows of 5 heads over 32768 int8 keys),
