@@ -13,7 +13,7 @@
 // and sines, one per thread, into LDS and then turns every head of q and k
 // with them: the double-precision work and the sine are paid once per token
 // and pair, not once per head.  Elements move 16 bytes a lane.  16384 tokens
-// of 40 + 8 heads of 128, out of a fused projection's rows: 81 us, 5.0 TB/s
+// of 40 + 8 heads of 128, out of a fused projection's rows: 73 us, 5.5 TB/s
 // (a plain copy of 1 GiB: 4.8); 8 tokens: 3.5 us, one workgroup's latency.
 #include "sc_internal.h"
 #include "sc_pool_view.h"
@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxHalf = 64;          // head_dim 128 / 2
-constexpr int kTokens = 4;            // tokens of a workgroup on long inputs: one angle per thread
+constexpr int kTokens = 16;           // tokens of a workgroup, at most
 
 // cos and sin of pair i at a position, amplitude included.
 __device__ __forceinline__ float2 angle_of(const RopeView &r, int32_t position, int i) {
@@ -193,10 +193,13 @@ hipError_t launch_rope(const RopeArgs &a, hipStream_t stream) {
   const int uq = rope_units(a.rope.half, a.rope.interleaved, a.dim_shift, a.in_place[0] != 0);
   const int uk = rope_units(a.rope.half, a.rope.interleaved, a.dim_shift, a.in_place[1] != 0);
   if (a.n_tokens <= 0 || a.heads[0] + a.heads[1] <= 0) return hipSuccess;
-  // One token per workgroup while that leaves CUs idle, else one angle per thread.
-  const int per = a.n_tokens <= 1024 ? 1 : kTokens;
+  // One token per workgroup while that leaves CUs idle; else as many as give
+  // every thread a unit.  16384 tokens of 40 heads of 128 (320 units) by one
+  // 58 us, by four 67; 65536 of 10 heads (80 units) by one 95, by four 59.
+  const int units = a.heads[0] * uq + a.heads[1] * uk;
+  const int per = a.n_tokens <= 1024 ? 1 : std::min(kTokens, (kThreads + units - 1) / std::max(1, units));
   // A launch's threads are counted in 32 bits.
-  constexpr int64_t kSlice = 1 << 25;
+  constexpr int64_t kSlice = 1 << 23;
   for (int64_t t0 = 0; t0 < a.n_tokens; t0 += kSlice) {
     RopeArgs b = a;
     b.n_tokens = (int32_t)std::min(kSlice, a.n_tokens - t0);
